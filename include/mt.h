@@ -436,6 +436,65 @@ int mt_op_attention(int32_t precision, const void* d_qkv, const int32_t* d_mask,
 int mt_op_layernorm(const float* d_x, const float* d_gamma, const float* d_beta, float eps, float* d_out_f32,
                     void* d_out_bf16, int32_t M, int32_t H, void* hip_stream);
 
+/*
+ * Operators on packed tokens: what the students of the merged model are trained with before they are merged (Sections 3.1 and 3.2: fine-tuning and
+ * distillation), and attention for prompts and single tokens of any length.  MT_BF16 (activations, weights and gradients bfloat16, sums float32) or
+ * MT_FP32_CHECK (all float32); other precisions: MT_ERR_CONFIG.  Tensors and row strides (in elements) are 16-byte aligned, workspaces 256-byte; a
+ * workspace holds nothing between calls, and calls that may overlap need one each.  hip_stream belongs to the current device.  No atomics on
+ * sums: equal inputs give equal bits.  Errors: NULL, CONFIG, SHAPE (also: a workspace smaller than the *_work function says), HIP.
+ */
+/* Attention over n_seqs packed sequences.  Sequence b owns query rows d_q_start[b] .. d_q_start[b+1]-1 and key rows d_k_start[b] .. d_k_start[b+1]-1
+ * (device int32 [n_seqs + 1], not falling; starts outside [0, total] are brought inside; d_k_start NULL: the queries').  With Lq queries and Lk keys,
+ * query i sees all Lk keys or, causal, the keys j <= i + Lk - Lq: the last query sees the last key, so a single token is a sequence of one query, and a
+ * prompt one of as many queries as keys.  Query head a reads key head a / (heads / kv_heads); heads % kv_heads == 0.
+ *   P = softmax(scale q k^T) over the keys seen, ctx = P v, lse = log sum exp(scale q k^T);  a query that sees no key: ctx 0, lse -infinity.
+ * Keys that a query does not see never reach it, whatever they hold; rows of no sequence are neither read nor written.
+ * Row r of head a of tensor t is `width` contiguous elements at t + r * t_row + a * t_head (results: rows within heads or heads within rows, none
+ * overlapping); width: a multiple of 8 up to 128; scale > 0.
+ * lse: float32 [heads][total_q].  MT_BF16 rounds P, and dS in the gradient, to bfloat16 where they enter the second products. */
+typedef struct mt_packed_attention {
+    const void *d_q, *d_k, *d_v;
+    void* d_ctx;
+    float* d_lse;                                   /* or NULL (mt_op_packed_attention only) */
+    const int32_t *d_q_start, *d_k_start;
+    const void* d_grad_ctx;                         /* these four: mt_op_packed_attention_grad only */
+    void *d_grad_q, *d_grad_k, *d_grad_v;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, ctx_row, ctx_head;
+    int64_t grad_ctx_row, grad_ctx_head, grad_q_row, grad_q_head, grad_k_row, grad_k_head, grad_v_row, grad_v_head;
+    int32_t precision, n_seqs, heads, kv_heads, width, total_q, total_k, causal;
+    float scale;
+    void* d_work;
+    size_t work_bytes;
+} mt_packed_attention;
+int mt_op_packed_attention(const mt_packed_attention* op, void* hip_stream);
+/* The gradients of q, k and v (of k and v summed over the heads that share them) from grad_ctx and mt_op_packed_attention's ctx and lse. */
+int mt_op_packed_attention_grad(const mt_packed_attention* op, void* hip_stream);
+/* Workspace bytes of either call (grad != 0: the second) for op's sizes; 0 if they are refused.  Host only. */
+size_t mt_op_packed_attention_work(const mt_packed_attention* op, int32_t grad);
+
+/* Softmax cross entropy of z = x W^T over a vocabulary, which never stores z.  d_x [tokens][ldx], d_W [vocab][ldw], hidden columns each (a multiple of
+ * 64); d_labels int32 [tokens]:  lse_i = log sum_v exp z_iv, loss_i = lse_i - z_i,label  (float32 [tokens], not averaged).  A label outside
+ * [0, vocab) means none: its token's row is not read, its loss and lse are 0, its gradient is 0. */
+int mt_op_vocab_loss(int32_t precision, const void* d_x, int64_t ldx, const void* d_W, int64_t ldw, const int32_t* d_labels, float* d_loss, float* d_lse,
+                     int32_t tokens, int32_t hidden, int32_t vocab, void* d_work, size_t work_bytes, void* hip_stream);
+/* dz_iv = weight_i (exp(z_iv - lse_i) - [v = label_i]), d_grad_x = dz W [tokens][hidden], d_grad_W = dz^T x [vocab][hidden] (dense, written whole;
+ * float32 with grad_W_f32 != 0).  d_lse: mt_op_vocab_loss's; d_weight float32 [tokens]: the gradient of each token's loss (1 / labelled tokens: their
+ * mean).  MT_BF16 rounds dz to bfloat16 where it enters the two products. */
+int mt_op_vocab_loss_grad(int32_t precision, const void* d_x, int64_t ldx, const void* d_W, int64_t ldw, const int32_t* d_labels, const float* d_lse,
+                          const float* d_weight, void* d_grad_x, void* d_grad_W, int32_t grad_W_f32, int32_t tokens, int32_t hidden, int32_t vocab,
+                          void* d_work, size_t work_bytes, void* hip_stream);
+size_t mt_op_vocab_loss_work(int32_t precision, int32_t tokens, int32_t hidden, int32_t vocab, int32_t grad);
+
+/* out_i = scale * table[id_i]; an id outside [0, vocab): a row of zeros.  hidden: a multiple of 8 (float32: of 4).  d_table [vocab][ldt], d_out [n][ldo]. */
+int mt_op_embedding(int32_t precision, const void* d_table, int64_t ldt, const int32_t* d_ids, float scale, void* d_out, int64_t ldo, int32_t n,
+                    int32_t vocab, int32_t hidden, void* hip_stream);
+/* The table's gradient: d_grad_table[v] = scale * sum over i with id_i = v of d_grad[i], float32 sums; zeros for rows without a token.
+ * out_f32 != 0 stores float32; accumulate != 0 (float32 only) adds to what is there instead and leaves other rows alone (a table that is also the
+ * classifier's weights: mt_op_vocab_loss_grad with grad_W_f32 first, then this). */
+int mt_op_embedding_grad(int32_t precision, const void* d_grad, int64_t ldg, const int32_t* d_ids, float scale, void* d_grad_table, int64_t ldt,
+                         int32_t out_f32, int32_t accumulate, int32_t n, int32_t vocab, int32_t hidden, void* d_work, size_t work_bytes, void* hip_stream);
+size_t mt_op_embedding_grad_work(int32_t precision, int32_t n, int32_t vocab, int32_t hidden);
+
 /* The FP8 contraction alone, as MT_FP8_FFN uses it: d_A [M][lda] and d_W [N][K] are E4M3 bytes (lda in elements, a
  * multiple of 16), C = act(scale * A W^T + bias) (+ residual); out_kind 0 bfloat16, 1 float32 (d_residual allowed, no
  * activation), 2 E4M3 (the value times out_scale, saturating).  act_kind 0 none, 1 GELU(erf), 2 GELU(tanh).

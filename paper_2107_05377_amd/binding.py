@@ -27,7 +27,9 @@ EXPORTS = ["mt_create", "mt_destroy", "mt_weight_bytes", "mt_workspace_bytes", "
            "mt_forward", "mt_logit_offset", "mt_n_logits", "mt_layer_count", "mt_last_error", "mt_error_name",
            "mt_read_hidden", "mt_profile_enable", "mt_profile_read", "mt_op_linear", "mt_op_attention",
            "mt_op_layernorm", "mt_op_linear_batched", "mt_debug_set_gemm_tile", "mt_share_weights", "mt_debug_mfma_peak", "mt_forward_typed", "mt_op_linear_sub", "mt_op_first_token_pool", "mt_op_panel_first_query", "mt_op_panel_first_attend", "mt_op_panel_first_attend_fp8", "mt_op_panel_linear", "mt_op_panel_linear_fp8", "mt_op_panel_attention", "mt_op_panel_layernorm", "mt_op_panel_layernorm_fp8", "mt_op_attention_fp8", "mt_schedule_steps", "mt_forward_routed",
-           "mt_forward_tokens", "mt_token_logit_offset", "mt_n_token_logits", "mt_forward_static", "mt_forward_multi", "mt_forward_requests", "mt_forward_routed_tokens", "mt_op_linear_fp8", "mt_debug_e4m3_quantize", "mt_check_mask"]
+           "mt_forward_tokens", "mt_token_logit_offset", "mt_n_token_logits", "mt_forward_static", "mt_forward_multi", "mt_forward_requests", "mt_forward_routed_tokens", "mt_op_linear_fp8", "mt_debug_e4m3_quantize", "mt_check_mask",
+           "mt_op_packed_attention", "mt_op_packed_attention_grad", "mt_op_packed_attention_work", "mt_op_vocab_loss", "mt_op_vocab_loss_grad",
+           "mt_op_vocab_loss_work", "mt_op_embedding", "mt_op_embedding_grad", "mt_op_embedding_grad_work"]
 MT_STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 
 
@@ -49,6 +51,13 @@ class mt_panel_linear(C.Structure):
                [(n, C.c_int64) for n in ("stride_A", "stride_W", "stride_bias", "stride_C", "sub_A", "sub_W", "sub_bias", "sub_C", "split_stride")] + \
                [(n, C.c_int32) for n in ("problems", "subs", "M", "N", "K", "lda", "ldw", "ldc", "act_kind", "out_f32", "splits", "transposed_from",
                                          "form", "height")]
+
+
+class mt_packed_attention(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_q", "d_k", "d_v", "d_ctx", "d_lse", "d_q_start", "d_k_start", "d_grad_ctx", "d_grad_q", "d_grad_k", "d_grad_v")] + \
+               [(n + part, C.c_int64) for n in ("q", "k", "v", "ctx", "grad_ctx", "grad_q", "grad_k", "grad_v") for part in ("_row", "_head")] + \
+               [(n, C.c_int32) for n in ("precision", "n_seqs", "heads", "kv_heads", "width", "total_q", "total_k", "causal")] + \
+               [("scale", C.c_float), ("d_work", C.c_void_p), ("work_bytes", C.c_size_t)]
 
 
 _lib = None
@@ -114,6 +123,16 @@ def lib():
         L.mt_op_panel_layernorm.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, i32, vp, i32, i32, vp]
         L.mt_op_linear_sub.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, i32, i32, i64, i64, i64, i64, vp, vp, i32, vp]
         L.mt_debug_set_gemm_tile.restype = i32
+        L.mt_op_packed_attention.argtypes = L.mt_op_packed_attention_grad.argtypes = [C.POINTER(mt_packed_attention), vp]
+        L.mt_op_packed_attention_work.argtypes = [C.POINTER(mt_packed_attention), i32]
+        L.mt_op_vocab_loss.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, sz, vp]
+        L.mt_op_vocab_loss_grad.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
+        L.mt_op_vocab_loss_work.argtypes = [i32, i32, i32, i32, i32]
+        L.mt_op_embedding.argtypes = [i32, vp, i64, vp, C.c_float, vp, i64, i32, i32, i32, vp]
+        L.mt_op_embedding_grad.argtypes = [i32, vp, i64, vp, C.c_float, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
+        L.mt_op_embedding_grad_work.argtypes = [i32, i32, i32, i32]
+        for f in (L.mt_op_packed_attention_work, L.mt_op_vocab_loss_work, L.mt_op_embedding_grad_work):
+            f.restype = sz
         _lib = L
     return _lib
 
@@ -562,6 +581,180 @@ def op_layernorm(x, gamma, beta, eps, want_bf16=False):
     if rc != MT_OK:
         raise MTError(rc, "mt_op_layernorm")
     return (of, ob) if want_bf16 else of
+
+
+def _refuse(bad, name, text):
+    if bad:
+        raise MTError(MT_ERR_SHAPE, f"{name}: {text}")
+
+
+def _act_type(name, precision):
+    import torch
+    if precision not in (MT_BF16, MT_FP32_CHECK):
+        raise MTError(MT_ERR_CONFIG, f"{name}: MT_BF16 or MT_FP32_CHECK")
+    return torch.bfloat16 if precision == MT_BF16 else torch.float32
+
+
+def _check_tensor(name, what, t, shape, dtype, device):
+    """A device tensor of `shape` (None: any size) and `dtype` on `device` whose last dimension is contiguous."""
+    _refuse(t.device.type != "cuda" or t.device != device, name, f"{what} is on {t.device}, the call on {device}")
+    _refuse(t.dtype != dtype, name, f"{what} is {t.dtype}, not {dtype}")
+    _refuse(t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)), name, f"{what} is {tuple(t.shape)}, not {shape}")
+    _refuse(t.stride(-1) != 1 and t.shape[-1] > 1, name, f"the last dimension of {what} is not contiguous")
+
+
+def _run(name, device, work_bytes, call):
+    """call(work pointer, work bytes, stream) with a workspace of its own, on `device` and its current stream."""
+    import torch
+    with torch.cuda.device(device):
+        work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None
+        rc = call(_ptr(work), work_bytes, _stream())
+    if rc != MT_OK:
+        raise MTError(rc, name)
+
+
+def _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale):
+    dt = _act_type(name, precision)
+    _refuse(q.dim() != 3 or k.dim() != 3, name, "q, k and v are [rows][heads][width]")
+    (tq, heads, d), (tk, kv_heads, _) = q.shape, k.shape
+    _check_tensor(name, "q", q, (tq, heads, d), dt, q.device)
+    _check_tensor(name, "k", k, (tk, kv_heads, d), dt, q.device)
+    _check_tensor(name, "v", v, (tk, kv_heads, d), dt, q.device)
+    import torch
+    _check_tensor(name, "q_start", q_start, (None,), torch.int32, q.device)
+    if k_start is not None:
+        _check_tensor(name, "k_start", k_start, tuple(q_start.shape), torch.int32, q.device)
+    op = mt_packed_attention(precision=precision, n_seqs=q_start.shape[0] - 1, heads=heads, kv_heads=kv_heads, width=d, total_q=tq, total_k=tk,
+                             causal=1 if causal else 0, scale=1.0 / float(d) ** 0.5 if scale is None else scale, d_q_start=q_start.data_ptr(),
+                             d_k_start=None if k_start is None else k_start.data_ptr())
+    for field, t in (("q", q), ("k", k), ("v", v)):
+        _set_rows(op, field, t)
+    return op, dt
+
+
+def _set_rows(op, field, t):
+    setattr(op, "d_" + field, t.data_ptr())
+    setattr(op, field + "_row", t.stride(0))
+    setattr(op, field + "_head", t.stride(1))
+
+
+def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, scale=None, out=None, want_lse=False):
+    """mt_op_packed_attention: q [queries][heads][width], k, v [keys][kv_heads][width] (any strides of rows and heads), q_start, k_start int32
+    [sequences + 1]; scale None: 1 / sqrt(width).  Returns the context [queries][heads][width] (`out`, or zeros where no sequence is) and with want_lse
+    the statistics [heads][queries] float32 for the gradient."""
+    import torch
+    name = "mt_op_packed_attention"
+    op, dt = _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale)
+    if out is None:
+        out = torch.zeros(tuple(q.shape), dtype=dt, device=q.device)
+    _check_tensor(name, "out", out, tuple(q.shape), dt, q.device)
+    _set_rows(op, "ctx", out)
+    lse = torch.full((q.shape[1], q.shape[0]), float("-inf"), dtype=torch.float32, device=q.device) if want_lse else None
+    op.d_lse = None if lse is None else lse.data_ptr()
+
+    def call(work, work_bytes, stream):
+        op.d_work, op.work_bytes = work, work_bytes
+        return lib().mt_op_packed_attention(C.byref(op), stream)
+    _run(name, q.device, lib().mt_op_packed_attention_work(C.byref(op), 0), call)
+    return (out, lse) if want_lse else out
+
+
+def op_packed_attention_grad(precision, grad_ctx, q, k, v, ctx, lse, q_start, k_start=None, causal=True, scale=None, out=None):
+    """mt_op_packed_attention_grad: the gradients of q, k and v (`out`, three tensors, or new ones with zeros where no sequence is) from grad_ctx and the
+    ctx and lse of op_packed_attention with the same arguments."""
+    import torch
+    name = "mt_op_packed_attention_grad"
+    op, dt = _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale)
+    _check_tensor(name, "grad_ctx", grad_ctx, tuple(q.shape), dt, q.device)
+    _check_tensor(name, "ctx", ctx, tuple(q.shape), dt, q.device)
+    _check_tensor(name, "lse", lse, (q.shape[1], q.shape[0]), torch.float32, q.device)
+    _refuse(not lse.is_contiguous(), name, "lse is not contiguous")
+    if out is None:
+        out = tuple(torch.zeros(tuple(t.shape), dtype=dt, device=q.device) for t in (q, k, v))
+    for what, t, like in zip(("grad_q", "grad_k", "grad_v"), out, (q, k, v)):
+        _check_tensor(name, what, t, tuple(like.shape), dt, q.device)
+        _set_rows(op, what, t)
+    _set_rows(op, "ctx", ctx)
+    _set_rows(op, "grad_ctx", grad_ctx)
+    op.d_lse = lse.data_ptr()
+
+    def call(work, work_bytes, stream):
+        op.d_work, op.work_bytes = work, work_bytes
+        return lib().mt_op_packed_attention_grad(C.byref(op), stream)
+    _run(name, q.device, lib().mt_op_packed_attention_work(C.byref(op), 1), call)
+    return tuple(out)
+
+
+def _vocab_loss(name, precision, x, W, labels):
+    import torch
+    dt = _act_type(name, precision)
+    _check_tensor(name, "x", x, (None, None), dt, x.device)
+    _check_tensor(name, "W", W, (None, x.shape[1]), dt, x.device)
+    _check_tensor(name, "labels", labels, (x.shape[0],), torch.int32, x.device)
+    return x.shape[0], x.shape[1], W.shape[0]
+
+
+def op_vocab_loss(precision, x, W, labels):
+    """mt_op_vocab_loss: x [tokens][hidden], W [vocab][hidden], labels int32 [tokens] (outside the vocabulary: none); returns the losses and the
+    statistics for the gradient, float32 [tokens] each."""
+    import torch
+    n, h, v = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
+    loss, lse = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
+    _run("mt_op_vocab_loss", x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
+        precision, _ptr(x), x.stride(0), _ptr(W), W.stride(0), _ptr(labels), _ptr(loss), _ptr(lse), n, h, v, work, size, stream))
+    return loss, lse
+
+
+def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
+    """mt_op_vocab_loss_grad: the gradients of x and of W (float32 with out_f32) for weight float32 [tokens], the gradient of each token's loss, and
+    op_vocab_loss's lse."""
+    import torch
+    name = "mt_op_vocab_loss_grad"
+    n, h, v = _vocab_loss(name, precision, x, W, labels)
+    _check_tensor(name, "lse", lse, (n,), torch.float32, x.device)
+    _check_tensor(name, "weight", weight, (n,), torch.float32, x.device)
+    dx = torch.empty((n, h), dtype=x.dtype, device=x.device)
+    dw = torch.empty((v, h), dtype=torch.float32 if out_f32 else x.dtype, device=x.device)
+    _run(name, x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 1), lambda work, size, stream: lib().mt_op_vocab_loss_grad(
+        precision, _ptr(x), x.stride(0), _ptr(W), W.stride(0), _ptr(labels), _ptr(lse), _ptr(weight), _ptr(dx), _ptr(dw), 1 if out_f32 else 0, n, h, v, work,
+        size, stream))
+    return dx, dw
+
+
+def op_embedding(precision, table, ids, scale=1.0, out=None):
+    """mt_op_embedding: scale * table[ids] for int32 ids [n]; rows of zeros for ids outside the table."""
+    import torch
+    name = "mt_op_embedding"
+    dt = _act_type(name, precision)
+    _check_tensor(name, "table", table, (None, None), dt, table.device)
+    _check_tensor(name, "ids", ids, (None,), torch.int32, table.device)
+    n, (v, h) = ids.shape[0], table.shape
+    if out is None:
+        out = torch.empty((n, h), dtype=dt, device=table.device)
+    _check_tensor(name, "out", out, (n, h), dt, table.device)
+    _run(name, table.device, 0, lambda work, size, stream: lib().mt_op_embedding(
+        precision, _ptr(table), table.stride(0), _ptr(ids), scale, _ptr(out), out.stride(0), n, v, h, stream))
+    return out
+
+
+def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add_to=None):
+    """mt_op_embedding_grad: the gradient of op_embedding's table [vocab][hidden] (float32 with out_f32); `add_to`: a float32 gradient that it is added
+    to instead."""
+    import torch
+    name = "mt_op_embedding_grad"
+    dt = _act_type(name, precision)
+    _check_tensor(name, "ids", ids, (None,), torch.int32, grad.device)
+    n, h = ids.shape[0], grad.shape[-1]
+    _check_tensor(name, "grad", grad, (n, h), dt, grad.device)
+    out = add_to
+    if out is None:
+        out = torch.empty((vocab, h), dtype=torch.float32 if out_f32 else dt, device=grad.device)
+    else:
+        _check_tensor(name, "add_to", out, (vocab, h), torch.float32, grad.device)
+    _run(name, grad.device, lib().mt_op_embedding_grad_work(precision, n, vocab, h), lambda work, size, stream: lib().mt_op_embedding_grad(
+        precision, _ptr(grad), grad.stride(0), _ptr(ids), scale, _ptr(out), out.stride(0), 1 if out.dtype == torch.float32 else 0,
+        0 if add_to is None else 1, n, vocab, h, work, size, stream))
+    return out
 
 
 def set_gemm_tile(sel: int) -> int:

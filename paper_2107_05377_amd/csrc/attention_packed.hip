@@ -1,0 +1,627 @@
+// Attention over packed sequences, causal or not, with grouped heads, and its gradient (bfloat16 and float32).
+//
+// Sequence b owns query rows q_start[b] .. q_start[b+1]-1 and key rows k_start[b] .. ; with Lq and Lk of them, query i sees the keys
+// j <= i + Lk - Lq (causal: the last query sees the last key) or all Lk.  Query head a reads key head a / group.
+//   S = scale q k^T,  lse = log sum_visible exp S,  P = exp(S - lse),  ctx = P v
+//   delta = dctx . ctx,  dS = P (dctx v^T - delta),  dv = P^T dctx,  dq = scale dS k,  dk = scale dS^T q
+//
+// Rows.  The query heads of a group share keys and values, so their rows are one list: row r of a (sequence, key head) is query r / group
+// of head r % group.  A group of 4 heads then needs its keys once, a single token has `group` rows, and dk, dv come out summed over the group.
+//
+// Matrix instructions: 32x32 blocks with float32 sums.  The forward pass and dq hold rows fixed and compute S^T = k q^T: a lane then holds ONE
+// row's scores of 16 of 32 keys, so that the softmax needs one exchange per block (with the other half of the wavefront), and P^T is in the
+// registers that the next product takes as its second operand.  The order of a sum is free, so the first operand (v^T or k^T, rows = head
+// columns) is read from the row-major LDS tile in the key order in which P^T lies: bfloat16 by transposing LDS reads, float32 by plain ones.
+// dk and dv hold keys fixed and compute S = q k^T, with the same step from S to the product over rows.
+//
+// Nothing that a row does not see reaches it: scores are replaced, not multiplied by zero, and in blocks that a mask cuts, a non-finite first
+// operand is kept out of the product and put back for the rows that see it.
+#include "packed_tile.h"
+#include "packed.h"
+
+#include <cmath>
+
+namespace mt {
+
+namespace {
+
+// the accumulators of a 32x32 block as the second operand of a product over its rows, step c
+__device__ __forceinline__ bf16x8 acc_frag(const f32x16& s, int c, B16)
+{
+    bf16x8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (__bf16)s[8 * c + j];
+    return f;
+}
+__device__ __forceinline__ f32x4 acc_frag(const f32x16& s, int c, F32)
+{
+    f32x4 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = s[4 * c + j];
+    return f;
+}
+
+// ---- non-finite operands of a block that a mask cuts
+// 0 where the element is finite, else a code: +inf 1, -inf 64, NaN 4096; sums of up to 32 codes are exact and tell which were among them
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bool split_bad(bf16x8& f, bf16x8& code)
+{
+    bool bad = false;
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    u16x8 v = __builtin_bit_cast(u16x8, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const bool b = (v[j] & 0x7F80) == 0x7F80;
+        code[j] = !b ? (__bf16)0.f : (v[j] & 0x7F) ? (__bf16)4096.f : (v[j] & 0x8000) ? (__bf16)64.f : (__bf16)1.f;
+        v[j] = b ? 0 : v[j];
+        bad |= b;
+    }
+    f = __builtin_bit_cast(bf16x8, v);
+    return bad;
+}
+__device__ __forceinline__ bool split_bad(f32x4& f, f32x4& code)
+{
+    bool bad = false;
+    u32x4 v = __builtin_bit_cast(u32x4, f);          // (of the whole vector: a bit cast of one element reads element 0)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool b = (v[j] & 0x7F800000u) == 0x7F800000u;
+        code[j] = !b ? 0.f : (v[j] & 0x7FFFFFu) ? 4096.f : (v[j] >> 31) ? 64.f : 1.f;
+        v[j] = b ? 0u : v[j];
+        bad |= b;
+    }
+    f = __builtin_bit_cast(f32x4, v);
+    return bad;
+}
+__device__ __forceinline__ bool any_bad(const bf16x8& f)
+{
+    const u32x4 v = __builtin_bit_cast(u32x4, f);
+    uint32_t t = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t |= (v[j] & 0x7F807F80u) + 0x00800080u;       // a full exponent carries into the sign's place
+    return (t & 0x80008000u) != 0;
+}
+__device__ __forceinline__ bool any_bad(const f32x4& f)
+{
+    const u32x4 v = __builtin_bit_cast(u32x4, f);
+    uint32_t t = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t |= (v[j] & 0x7F800000u) + 0x00800000u;
+    return (t >> 31) != 0;
+}
+
+// acc += (columns of the tile) x w, w the accumulators of a block of 32 rows (in the sum) whose element i is nonzero only where bit i of `seen`
+// is set; `cut`: some are not set.  w carries a sign (dS) or not (P): an infinity is put back with its own sign only for P, as NaN for dS.
+template <typename E, int DP, bool SIGNED>
+__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsigned char* t, int row0, const f32x16& w, bool cut, uint32_t seen, int lane)
+{
+    using T = Tile<E, DP>;
+    constexpr int STEPS = 32 / E::KS;
+    typename E::frag wf[STEPS];
+#pragma unroll
+    for (int c = 0; c < STEPS; ++c) wf[c] = acc_frag(w, c, E{});
+    if (!cut) {
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) acc[db] = E::mma(T::col_frag(t, row0, db, c, lane), wf[c], acc[db]);
+        return;
+    }
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db) {
+        typename E::frag a[STEPS];
+        bool bad = false;
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) {
+            a[c] = T::col_frag(t, row0, db, c, lane);
+            bad |= any_bad(a[c]);
+        }
+        if (__any(bad)) {
+            f32x16 code;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) code[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) {
+                typename E::frag m, one;
+                split_bad(a[c], m);
+                f32x16 s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = (seen >> i) & 1 ? 1.f : 0.f;
+                one = acc_frag(s, c, E{});
+                code = E::mma(m, one, code);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = (int)code[i];
+                const bool up = (n & 63) != 0, down = (n & 4032) != 0;
+                const float put = (SIGNED || n >= 4096 || (up && down)) ? NAN : up ? INFINITY : -INFINITY;
+                acc[db][i] += n ? put : 0.f;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) acc[db] = E::mma(a[c], wf[c], acc[db]);
+    }
+}
+
+// ---- sequences
+struct Seq {
+    int q0, lq, k0, lk, tile;
+};
+__device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v, 0), total); }
+
+// The sequence and tile that workgroup w of a list of tiles (`tile` rows each, `per` rows per token, of the queries or of the keys) works on; false
+// behind the last.  Starts outside the arrays are brought inside, a sequence that would end before it starts is empty.
+__device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, int tile, bool keys, Seq& s)
+{
+    const int lane = threadIdx.x & 63;
+    const int32_t* start = keys ? p.k_start : p.q_start;
+    const int total = keys ? p.total_k : p.total_q;
+    int base = 0;
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
+        const int b = min(b0 + lane, p.n_seqs - 1);
+        const int a = clamp_start(start[b], total), e = clamp_start(start[b + 1], total);
+        const int n = b0 + lane < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(sum, o);
+            if (lane >= o) sum += up;
+        }
+        const int all = __shfl(sum, 63);
+        if (w < base + all) {
+            const uint64_t past = __ballot(base + sum > w);
+            const int l = __ffsll((unsigned long long)past) - 1;
+            const int bb = b0 + l;
+            const int first = base + __shfl(sum, l) - __shfl(n, l);
+            s.tile = w - first;
+            s.q0 = clamp_start(p.q_start[bb], p.total_q);
+            s.lq = max(clamp_start(p.q_start[bb + 1], p.total_q) - s.q0, 0);
+            s.k0 = clamp_start(p.k_start[bb], p.total_k);
+            s.lk = max(clamp_start(p.k_start[bb + 1], p.total_k) - s.k0, 0);
+            return true;
+        }
+        base += all;
+    }
+    return false;
+}
+
+// rows row0 .. row0 + ROWS - 1 (none beyond `last`, whose copy stands in) of a matrix into an LDS tile, 16 bytes a lane straight from memory.
+// Columns beyond the head's width hold copies of the first ones: they meet zeros, or results that nobody stores.
+template <typename E, int DP, int ROWS, int NW, bool GROUPED>
+__device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_stride, int64_t head_stride, int group, int row0, int last, int d, unsigned char* t)
+{
+    using T = Tile<E, DP>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int N = ROWS / T::RPI;
+    static_assert(N % NW == 0, "rows must split evenly over wavefront loads");
+#pragma unroll
+    for (int i = 0; i < N / NW; ++i) {
+        const int blk = __builtin_amdgcn_readfirstlane(wave + i * NW);
+        const int row = blk * T::RPI + lane / T::CH;
+        int chunk = (lane % T::CH) ^ T::key(row);
+        if (chunk * E::EPC >= d) chunk = 0;
+        const int r = min(row0 + row, last);
+        const typename E::elem* at;
+        if constexpr (GROUPED) {
+            const int tok = r / group;
+            at = base + tok * row_stride + (r - tok * group) * head_stride;
+        } else at = base + r * row_stride;
+        __builtin_amdgcn_global_load_lds((gptr_t)(at + chunk * E::EPC), (lptr_t)(t + blk * 1024), 16, 0, 0);
+    }
+}
+
+__device__ __forceinline__ void loads_landed()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+template <typename E, int DP>
+__device__ __forceinline__ void load_row(typename E::frag (&f)[DP / E::KS], const typename E::elem* row, int d, int half)
+{
+#pragma unroll
+    for (int ks = 0; ks < DP / E::KS; ++ks) {
+        const int c = ks * E::KS + half * E::EPC;
+#pragma unroll
+        for (int j = 0; j < E::EPC; ++j) f[ks][j] = (typename E::elem)0.f;
+        if (c < d) f[ks] = *reinterpret_cast<const typename E::frag*>(row + c);
+    }
+}
+
+template <typename E, int DP>
+__device__ __forceinline__ void store_cols(const f32x16 (&acc)[DP / 32], float by, typename E::elem* row, int d, int half)
+{
+    typedef typename E::elem out4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = db * 32 + g * 8 + half * 4;
+            if (c >= d) continue;
+            out4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = (typename E::elem)(acc[db][g * 4 + j] * by);
+            *reinterpret_cast<out4*>(row + c) = v;
+        }
+}
+
+constexpr int kTileKeys = 64;
+
+template <typename E, int DP, int NW>
+__global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
+{
+    using T = Tile<E, DP>;
+    typedef typename E::elem elem;
+    constexpr int BM = NW * 32, TK = kTileKeys, BYTES = TK * T::ROWB;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of keys and values
+    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    Seq s;
+    if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
+    const int r0 = (tiles - 1 - s.tile) * BM;                                 // the rows that see most first
+    const int shift = p.causal ? s.lk - s.lq : 0x40000000;                    // query i sees keys up to i + shift
+    const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
+    const int my_row = min(r0 + wave * 32 + l32, rows - 1);
+    const int tok = my_row / group, head = kvh * group + my_row - tok * group;
+    const int limit = limit_of(my_row), wave_min = limit_of(r0 + wave * 32), wave_max = limit_of(r0 + wave * 32 + 31);
+    const int n_keys = limit_of(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
+
+    const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
+    const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    typename E::frag qf[DP / E::KS];
+    load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+    const float c = p.scale * kLog2e;
+    float ref = -INFINITY, sum = 0.f;       // weights are exp2(c (score - ref))
+
+    if (n_tiles > 0) {
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds + BYTES);
+    }
+    for (int kt = 0; kt < n_tiles; ++kt) {
+        loads_landed();
+        const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
+        const unsigned char* tv = tk + BYTES;
+        if (kt + 1 < n_tiles) {
+            unsigned char* next = lds + ((kt + 1) & 1) * 2 * BYTES;
+            stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
+            stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
+        }
+        const int key0 = kt * TK;
+        if (key0 > wave_max) continue;
+        f32x16 sc[TK / 32];
+#pragma unroll
+        for (int u = 0; u < TK / 32; ++u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < DP / E::KS; ++ks) sc[u] = E::mma(T::row_frag(tk, u * 32 + l32, ks, half), qf[ks], sc[u]);
+        }
+        const bool cut = key0 + TK - 1 > wave_min;
+        uint32_t seen[TK / 32];
+        if (cut) {
+#pragma unroll
+            for (int u = 0; u < TK / 32; ++u) {
+                seen[u] = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool see = key0 + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit;
+                    seen[u] |= see ? 1u << i : 0u;
+                    sc[u][i] = see ? sc[u][i] : -INFINITY;
+                }
+            }
+        }
+        float top = sc[0][0];
+#pragma unroll
+        for (int u = 0; u < TK / 32; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
+        top = lane_pair_max<32>(top);
+        // the reference follows the maximum only when that has grown by 2^8: the weights' sums stay far from overflow and the accumulators are
+        // rescaled a few times per row instead of once per tile
+        if (__any((top - ref) * c > 8.f || ref == -INFINITY)) {
+            const float to = fmaxf(ref, top);
+            const float by = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ref - to) * c);
+            ref = to;
+            sum *= by;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] *= by;
+        }
+        const float rc = ref == -INFINITY ? 0.f : ref * c;
+#pragma unroll
+        for (int u = 0; u < TK / 32; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                sc[u][i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i], c, -rc));
+                sum += sc[u][i];
+            }
+#pragma unroll
+        for (int u = 0; u < TK / 32; ++u) add_product<E, DP, false>(acc, tv, u * 32, sc[u], cut, seen[u], lane);
+    }
+    sum = lane_pair_sum<32>(sum);
+    if (r0 + wave * 32 + l32 < rows) {
+        const float by = limit < 0 ? 0.f : 1.f / sum;
+        if (limit < 0) {
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+        }
+        store_cols<E, DP>(acc, by, static_cast<elem*>(p.out) + (int64_t)(s.q0 + tok) * p.o_row + head * p.o_head, p.d, half);
+        if (p.lse && half == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
+    }
+}
+
+// delta = dctx . ctx per (head, query): one wavefront per 8 rows, 8 lanes a row
+template <typename E>
+__global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* delta)
+{
+    typedef typename E::elem elem;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int part = threadIdx.x & 7;
+    if (at >= (int64_t)p.total_q * p.heads) return;
+    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads);
+    const elem* o = static_cast<const elem*>(p.ctx) + row * p.o_row + head * p.o_head;
+    const elem* g = static_cast<const elem*>(p.dctx) + row * p.g_row + head * p.g_head;
+    float sum = 0.f;
+    for (int c = part * E::EPC; c < p.d; c += 8 * E::EPC) {
+        const typename E::frag a = *reinterpret_cast<const typename E::frag*>(o + c), b = *reinterpret_cast<const typename E::frag*>(g + c);
+#pragma unroll
+        for (int j = 0; j < E::EPC; ++j) sum = fmaf((float)a[j], (float)b[j], sum);
+    }
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    sum += __shfl_xor(sum, 4);
+    if (part == 0) delta[(int64_t)head * p.total_q + row] = sum;
+}
+
+// dq: rows fixed, keys pass by
+template <typename E, int DP, int NW>
+__global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const float* delta)
+{
+    using T = Tile<E, DP>;
+    typedef typename E::elem elem;
+    constexpr int BM = NW * 32, TK = 32, BYTES = TK * T::ROWB;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    Seq s;
+    if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
+    const int r0 = (tiles - 1 - s.tile) * BM;
+    const int shift = p.causal ? s.lk - s.lq : 0x40000000;
+    const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
+    const int my_row = min(r0 + wave * 32 + l32, rows - 1);
+    const int tok = my_row / group, head = kvh * group + my_row - tok * group;
+    const int limit = limit_of(my_row), wave_min = limit_of(r0 + wave * 32), wave_max = limit_of(r0 + wave * 32 + 31);
+    const int n_keys = limit_of(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
+
+    const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
+    const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    typename E::frag qf[DP / E::KS], gf[DP / E::KS];
+    load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
+    load_row<E, DP>(gf, static_cast<const elem*>(p.dctx) + (int64_t)(s.q0 + tok) * p.g_row + head * p.g_head, p.d, half);
+    const float c = p.scale * kLog2e;
+    const float lse = p.lse_in[(int64_t)head * p.total_q + s.q0 + tok] * kLog2e, dl = delta[(int64_t)head * p.total_q + s.q0 + tok];
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+    if (n_tiles > 0) {
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds + BYTES);
+    }
+    for (int kt = 0; kt < n_tiles; ++kt) {
+        loads_landed();
+        const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
+        const unsigned char* tv = tk + BYTES;
+        if (kt + 1 < n_tiles) {
+            unsigned char* next = lds + ((kt + 1) & 1) * 2 * BYTES;
+            stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
+            stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
+        }
+        const int key0 = kt * TK;
+        if (key0 > wave_max) continue;
+        f32x16 sc, dp;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < DP / E::KS; ++ks) {
+            sc = E::mma(T::row_frag(tk, l32, ks, half), qf[ks], sc);
+            dp = E::mma(T::row_frag(tv, l32, ks, half), gf[ks], dp);
+        }
+        const bool cut = key0 + TK - 1 > wave_min;
+        uint32_t seen = 0xFFFFu;
+        if (cut) {
+            seen = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) seen |= key0 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? 1u << i : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
+            sc[i] = (seen >> i) & 1 ? w : 0.f;
+        }
+        add_product<E, DP, true>(acc, tk, 0, sc, cut, seen, lane);
+    }
+    if (r0 + wave * 32 + l32 < rows)
+        store_cols<E, DP>(acc, p.scale, static_cast<elem*>(p.dq) + (int64_t)(s.q0 + tok) * p.dq_row + head * p.dq_head, p.d, half);
+}
+
+// dk, dv: keys fixed, the rows of all heads of the group pass by
+template <typename E, int DP, int NW>
+__global__ __launch_bounds__(NW * 64) void packed_dkv_kernel(PackedAttn p, const float* delta)
+{
+    using T = Tile<E, DP>;
+    typedef typename E::elem elem;
+    constexpr int BN = NW * 32, TQ = 32, BYTES = TQ * T::ROWB;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of rows of q and dctx; their statistics
+    struct RowInfo {
+        float lse[TQ], delta[TQ];
+        int limit[TQ];
+    };
+    RowInfo* const info = reinterpret_cast<RowInfo*>(lds + 4 * BYTES);
+    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    Seq s;
+    if (!find_tile(p, blockIdx.x, 1, BN, true, s)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rows = s.lq * group, n0 = s.tile * BN;
+    const int shift = p.causal ? s.lk - s.lq : 0x40000000;
+    const int my_key = n0 + wave * 32 + l32, key = min(my_key, s.lk - 1);
+    const int wave_last = min(n0 + wave * 32 + 31, s.lk - 1), wave_first = n0 + wave * 32;
+    // the first query that sees the tile's first key
+    const int t_first = p.causal ? min(max(n0 - shift, 0), s.lq) : 0;
+    const int rt0 = t_first * group / TQ, n_tiles = (rows + TQ - 1) / TQ;
+
+    typename E::frag kf[DP / E::KS], vf[DP / E::KS];
+    load_row<E, DP>(kf, static_cast<const elem*>(p.k) + (int64_t)(s.k0 + key) * p.k_row + kvh * p.k_head, p.d, half);
+    load_row<E, DP>(vf, static_cast<const elem*>(p.v) + (int64_t)(s.k0 + key) * p.v_row + kvh * p.v_head, p.d, half);
+    const elem* Q = static_cast<const elem*>(p.q) + (int64_t)s.q0 * p.q_row + (int64_t)kvh * group * p.q_head;
+    const elem* G = static_cast<const elem*>(p.dctx) + (int64_t)s.q0 * p.g_row + (int64_t)kvh * group * p.g_head;
+    const float c = p.scale * kLog2e;
+
+    f32x16 ak[DP / 32], av[DP / 32];
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ak[db][i] = av[db][i] = 0.f;
+
+    float r_lse = 0.f, r_delta = 0.f;
+    int r_limit = -1;
+    const auto fetch = [&](int rt, unsigned char* to) {
+        stage<E, DP, TQ, NW, true>(Q, p.q_row, p.q_head, group, rt * TQ, rows - 1, p.d, to);
+        stage<E, DP, TQ, NW, true>(G, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
+        if (threadIdx.x < TQ) {
+            const int r = rt * TQ + threadIdx.x, rr = min(r, rows - 1), t = rr / group;
+            const int64_t at = (int64_t)(kvh * group + rr - t * group) * p.total_q + s.q0 + t;
+            r_lse = p.lse_in[at] * kLog2e;
+            r_delta = delta[at];
+            r_limit = r < rows ? min(t + shift, s.lk - 1) : -1;
+        }
+    };
+    const auto keep = [&](RowInfo& i) {
+        if (threadIdx.x < TQ) {
+            i.lse[threadIdx.x] = r_lse;
+            i.delta[threadIdx.x] = r_delta;
+            i.limit[threadIdx.x] = r_limit;
+        }
+    };
+    if (rt0 < n_tiles) {
+        fetch(rt0, lds);
+        keep(info[0]);
+    }
+    for (int rt = rt0; rt < n_tiles; ++rt) {
+        loads_landed();
+        const int at = (rt - rt0) & 1;
+        const unsigned char* tq = lds + at * 2 * BYTES;
+        const unsigned char* tg = tq + BYTES;
+        const RowInfo& in = info[at];
+        const bool more = rt + 1 < n_tiles;
+        if (more) fetch(rt + 1, lds + (at ^ 1) * 2 * BYTES);
+        // the tile's last row sees most
+        const int last_limit = min(min((rt * TQ + TQ - 1), rows - 1) / group + shift, s.lk - 1), first_limit = min(rt * TQ / group + shift, s.lk - 1);
+        if (wave_first <= last_limit) {
+            f32x16 sc, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < DP / E::KS; ++ks) {
+                sc = E::mma(T::row_frag(tq, l32, ks, half), kf[ks], sc);
+                dp = E::mma(T::row_frag(tg, l32, ks, half), vf[ks], dp);
+            }
+            const bool cut = wave_last > first_limit || rt * TQ + TQ > rows;
+            uint32_t seen = 0xFFFFu;
+            if (cut) {
+                seen = 0;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[8 * g + 4 * half]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * g + j;
+                    const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -l[j]));
+                    const float ds = w * (dp[i] - dl[j]);
+                    sc[i] = (seen >> i) & 1 ? w : 0.f;
+                    dp[i] = (seen >> i) & 1 ? ds : 0.f;
+                }
+            }
+            add_product<E, DP, false>(av, tg, 0, sc, cut, seen, lane);
+            add_product<E, DP, true>(ak, tq, 0, dp, cut, seen, lane);
+        }
+        if (more) keep(info[at ^ 1]);
+    }
+    if (my_key < s.lk) {
+        store_cols<E, DP>(ak, p.scale, static_cast<elem*>(p.dk) + (int64_t)(s.k0 + key) * p.dk_row + kvh * p.dk_head, p.d, half);
+        store_cols<E, DP>(av, 1.f, static_cast<elem*>(p.dv) + (int64_t)(s.k0 + key) * p.dv_row + kvh * p.dv_head, p.d, half);
+    }
+}
+
+template <typename E, int DP, int NW>
+hipError_t forward_with(const PackedAttn& p, hipStream_t stream)
+{
+    static std::atomic<uint64_t> done{0};
+    const int bytes = 4 * kTileKeys * Tile<E, DP>::ROWB;
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, NW>), bytes, done);
+    if (e != hipSuccess) return e;
+    const int64_t tiles = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
+    if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
+    packed_forward_kernel<E, DP, NW><<<dim3((unsigned)tiles, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <typename E, int DP>
+hipError_t gradient_with(const PackedAttn& p, hipStream_t stream)
+{
+    constexpr int NW = 4;
+    static std::atomic<uint64_t> done_q{0}, done_k{0};
+    const int bytes = 4 * 32 * Tile<E, DP>::ROWB, bytes_k = bytes + 2 * 32 * 12;
+    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, NW>), bytes, done_q);
+    if (e != hipSuccess) return e;
+    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, NW>), bytes_k, done_k);
+    if (e != hipSuccess) return e;
+    float* delta = static_cast<float*>(p.work);
+    const int64_t n = (int64_t)p.total_q * p.heads;
+    const int64_t tiles_q = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
+    const int64_t tiles_k = ((int64_t)p.total_k + NW * 32 - 1) / (NW * 32) + p.n_seqs;
+    if (tiles_q > 0x7FFFFFFF || tiles_k > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, delta);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    packed_dkv_kernel<E, DP, NW><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), NW * 64, bytes_k, stream>>>(p, delta);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    packed_dq_kernel<E, DP, NW><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p, delta);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t packed_attention_work(int, int, int, int, int, int, int) { return 0; }
+size_t packed_attention_grad_work(int total_q, int heads) { return (size_t)total_q * heads * 4; }
+
+hipError_t launch_packed_attention(const PackedAttn& p, int f32, hipStream_t stream)
+{
+    if (f32) return p.d <= 64 ? forward_with<F32, 64, 4>(p, stream) : forward_with<F32, 128, 4>(p, stream);
+    return p.d <= 64 ? forward_with<B16, 64, 4>(p, stream) : forward_with<B16, 128, 4>(p, stream);
+}
+
+hipError_t launch_packed_attention_grad(const PackedAttn& p, int f32, hipStream_t stream)
+{
+    if (f32) return p.d <= 64 ? gradient_with<F32, 64>(p, stream) : gradient_with<F32, 128>(p, stream);
+    return p.d <= 64 ? gradient_with<B16, 64>(p, stream) : gradient_with<B16, 128>(p, stream);
+}
+
+}  // namespace mt
