@@ -583,39 +583,48 @@ def op_layernorm(x, gamma, beta, eps, want_bf16=False):
     return (of, ob) if want_bf16 else of
 
 
-def _refuse(bad, name, text):
-    if bad:
-        raise MTError(MT_ERR_SHAPE, f"{name}: {text}")
+def _refuse(name, text, code=MT_ERR_SHAPE):
+    raise MTError(code, f"{name}: {text}")
 
 
 def _act_type(name, precision):
     import torch
-    if precision not in (MT_BF16, MT_FP32_CHECK):
-        raise MTError(MT_ERR_CONFIG, f"{name}: MT_BF16 or MT_FP32_CHECK")
-    return torch.bfloat16 if precision == MT_BF16 else torch.float32
+    if precision == MT_BF16:
+        return torch.bfloat16
+    if precision != MT_FP32_CHECK:
+        _refuse(name, "MT_BF16 or MT_FP32_CHECK", MT_ERR_CONFIG)
+    return torch.float32
 
 
 def _check_tensor(name, what, t, shape, dtype, device):
-    """A device tensor of `shape` (None: any size) and `dtype` on `device` whose last dimension is contiguous."""
-    _refuse(t.device.type != "cuda" or t.device != device, name, f"{what} is on {t.device}, the call on {device}")
-    _refuse(t.dtype != dtype, name, f"{what} is {t.dtype}, not {dtype}")
-    _refuse(t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)), name, f"{what} is {tuple(t.shape)}, not {shape}")
-    _refuse(t.stride(-1) != 1 and t.shape[-1] > 1, name, f"the last dimension of {what} is not contiguous")
+    """A tensor of `shape` (None: any) and `dtype` on the call's device, whose last dimension is contiguous."""
+    if t.device != device or device.type != "cuda":
+        _refuse(name, f"{what} is on {t.device}, the call on {device}: all tensors of a call are on one GPU")
+    if t.dtype != dtype:
+        _refuse(name, f"{what} is {t.dtype}, not {dtype}")
+    have = tuple(t.shape)
+    if have != shape and (len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have))):
+        _refuse(name, f"{what} is {have}, not {shape}")
+    if have[-1] > 1 and t.stride(-1) != 1:
+        _refuse(name, f"the last dimension of {what} is not contiguous")
 
 
 def _run(name, device, work_bytes, call):
     """call(work pointer, work bytes, stream) with a workspace of its own, on `device` and its current stream."""
     import torch
-    with torch.cuda.device(device):
-        work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None
-        rc = call(_ptr(work), work_bytes, _stream())
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run(name, device, work_bytes, call)
+    work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None
+    rc = call(work.data_ptr() if work_bytes else None, work_bytes, torch.cuda.current_stream(device).cuda_stream)
     if rc != MT_OK:
         raise MTError(rc, name)
 
 
 def _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale):
     dt = _act_type(name, precision)
-    _refuse(q.dim() != 3 or k.dim() != 3, name, "q, k and v are [rows][heads][width]")
+    if q.dim() != 3 or k.dim() != 3:
+        _refuse(name, "q, k and v are [rows][heads][width]")
     (tq, heads, d), (tk, kv_heads, _) = q.shape, k.shape
     _check_tensor(name, "q", q, (tq, heads, d), dt, q.device)
     _check_tensor(name, "k", k, (tk, kv_heads, d), dt, q.device)
@@ -668,7 +677,8 @@ def op_packed_attention_grad(precision, grad_ctx, q, k, v, ctx, lse, q_start, k_
     _check_tensor(name, "grad_ctx", grad_ctx, tuple(q.shape), dt, q.device)
     _check_tensor(name, "ctx", ctx, tuple(q.shape), dt, q.device)
     _check_tensor(name, "lse", lse, (q.shape[1], q.shape[0]), torch.float32, q.device)
-    _refuse(not lse.is_contiguous(), name, "lse is not contiguous")
+    if not lse.is_contiguous():
+        _refuse(name, "lse is not contiguous")
     if out is None:
         out = tuple(torch.zeros(tuple(t.shape), dtype=dt, device=q.device) for t in (q, k, v))
     for what, t, like in zip(("grad_q", "grad_k", "grad_v"), out, (q, k, v)):
@@ -701,7 +711,7 @@ def op_vocab_loss(precision, x, W, labels):
     n, h, v = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
     loss, lse = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
     _run("mt_op_vocab_loss", x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
-        precision, _ptr(x), x.stride(0), _ptr(W), W.stride(0), _ptr(labels), _ptr(loss), _ptr(lse), n, h, v, work, size, stream))
+        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), n, h, v, work, size, stream))
     return loss, lse
 
 
@@ -716,7 +726,7 @@ def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
     dx = torch.empty((n, h), dtype=x.dtype, device=x.device)
     dw = torch.empty((v, h), dtype=torch.float32 if out_f32 else x.dtype, device=x.device)
     _run(name, x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 1), lambda work, size, stream: lib().mt_op_vocab_loss_grad(
-        precision, _ptr(x), x.stride(0), _ptr(W), W.stride(0), _ptr(labels), _ptr(lse), _ptr(weight), _ptr(dx), _ptr(dw), 1 if out_f32 else 0, n, h, v, work,
+        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), lse.data_ptr(), weight.data_ptr(), dx.data_ptr(), dw.data_ptr(), 1 if out_f32 else 0, n, h, v, work,
         size, stream))
     return dx, dw
 
@@ -733,7 +743,7 @@ def op_embedding(precision, table, ids, scale=1.0, out=None):
         out = torch.empty((n, h), dtype=dt, device=table.device)
     _check_tensor(name, "out", out, (n, h), dt, table.device)
     _run(name, table.device, 0, lambda work, size, stream: lib().mt_op_embedding(
-        precision, _ptr(table), table.stride(0), _ptr(ids), scale, _ptr(out), out.stride(0), n, v, h, stream))
+        precision, table.data_ptr(), table.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), n, v, h, stream))
     return out
 
 
@@ -752,7 +762,7 @@ def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add
     else:
         _check_tensor(name, "add_to", out, (vocab, h), torch.float32, grad.device)
     _run(name, grad.device, lib().mt_op_embedding_grad_work(precision, n, vocab, h), lambda work, size, stream: lib().mt_op_embedding_grad(
-        precision, _ptr(grad), grad.stride(0), _ptr(ids), scale, _ptr(out), out.stride(0), 1 if out.dtype == torch.float32 else 0,
+        precision, grad.data_ptr(), grad.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), 1 if out.dtype == torch.float32 else 0,
         0 if add_to is None else 1, n, vocab, h, work, size, stream))
     return out
 

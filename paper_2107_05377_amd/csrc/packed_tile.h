@@ -38,7 +38,8 @@ struct Tile {
     static constexpr int ROWB = DP * E::SIZE, CH = ROWB / 16, RPI = 1024 / ROWB;
     static __device__ __forceinline__ int key(int row)
     {
-        if constexpr (CH == 8) return ((row >> 3) & 1) | ((row >> 1) & 2) | ((row << 1) & 4);       // the row pair's three bits reversed
+        if constexpr (CH == 4) return (row >> 2) & 3;
+        else if constexpr (CH == 8) return ((row >> 3) & 1) | ((row >> 1) & 2) | ((row << 1) & 4);       // the row pair's three bits reversed
         else if constexpr (E::SIZE == 2) return ((row & 3) << 2) | ((row >> 2) & 3);
         else return (row & 3) | ((row << 1) & 8) | ((row >> 1) & 4);
     }

@@ -9,14 +9,14 @@
 #include "packed_tile.h"
 #include "packed.h"
 
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace mt {
 
 namespace {
 
-constexpr int kTok = 128, kVoc = 128;       // tile of the products
-constexpr int kPieceGrain = 256;
 
 // ---- the labelled tokens, in order: index[0 .. *count)
 __global__ __launch_bounds__(1024) void label_index_kernel(const int32_t* labels, int tokens, int vocab, int32_t* count, int32_t* index)
@@ -54,12 +54,12 @@ struct Operand {
     int32_t k_n;                // column operand: rows that exist; the last one stands in for those beyond, which must meet zeros
 };
 
-template <typename E, int B, int NW, bool COLS>
+template <typename E, int B, int BK, int NW, bool COLS>
 struct Stager {
-    static constexpr int BK = 128 / E::SIZE;                        // elements of the sum per slice
     static constexpr int WIDTH = COLS ? B : BK, ROWS = COLS ? BK : B;
     using T = Tile<E, WIDTH>;
     static constexpr int BYTES = ROWS * T::ROWB, N = BYTES / 1024 / NW;
+    static_assert(N * NW * 1024 == BYTES, "a tile must split evenly over wavefront loads");
     const typename E::elem* at[N];
     int64_t ld;
     int row[N];
@@ -98,87 +98,156 @@ struct Stager {
     }
 };
 
-// acc[i][j]: block i of the first operand's rows (registers) and j of the second's (lanes); 4 wavefronts, 64 x 64 each
-template <typename E, bool ACOL, bool BCOL>
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// A workgroup's BM x BN block of a product: WM x WN wavefronts of TMI x TNI blocks of 32 x 32; acc[i][j]: block i of the first operand's rows (registers),
+// j of the second's (lanes).  Slices of BK elements of the sum go through a ring of STAGES in LDS, straight from memory; the barrier of a slice stands in
+// its last step, when its operands are in registers, so that the next slice's first operands are read behind that step's matrix instructions.
+template <typename E, bool ACOL, bool BCOL, int WM, int WN, int TMI, int TNI, int BK, int STAGES>
 struct Product {
-    static constexpr int B = 128, NW = 4;
-    using SA = Stager<E, B, NW, ACOL>;
-    using SB = Stager<E, B, NW, BCOL>;
-    static constexpr int BK = SA::BK, STEPS = BK / E::KS, LDS = 2 * (SA::BYTES + SB::BYTES);
+    static constexpr int BM = WM * TMI * 32, BN = WN * TNI * 32, NW = WM * WN, NT = NW * 64;
+    using SA = Stager<E, BM, BK, NW, ACOL>;
+    using SB = Stager<E, BN, BK, NW, BCOL>;
+    static constexpr int STAGE = SA::BYTES + SB::BYTES, STEPS = BK / E::KS, LDS = STAGES * STAGE, LPS = SA::N + SB::N;
+    static constexpr int kBK = BK, tmi = TMI, tni = TNI;
+    static_assert(LDS <= 160 * 1024 && STAGES >= 2 && LPS * (STAGES - 2) < 64, "");
+
+    static __device__ __forceinline__ void wait_slices(int n)       // all but the last n slices issued have landed
+    {
+        if (STAGES >= 4 && n >= 2) wait_loads<2 * LPS>();
+        else if (STAGES >= 3 && n >= 1) wait_loads<LPS>();
+        else wait_loads<0>();
+    }
+    static __device__ __forceinline__ int wave_m() { return (threadIdx.x >> 6) / WN * TMI * 32; }
+    static __device__ __forceinline__ int wave_n() { return (threadIdx.x >> 6) % WN * TNI * 32; }
 
     // sums over [k0, k1): k0 a multiple of BK; row operands hold whole slices
-    static __device__ __forceinline__ void run(f32x16 (&acc)[2][2], const Operand& a, int a0, const Operand& b, int b0, int k0, int k1, unsigned char* lds)
+    static __device__ __forceinline__ void run(f32x16 (&acc)[TMI][TNI], const Operand& a, int a0, const Operand& b, int b0, int k0, int k1, unsigned char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-        const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+        static_assert(STAGES <= 4, "wait_slices");
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+        const int wm = wave / WN * TMI * 32, wn = wave % WN * TNI * 32;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TMI; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < TNI; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        const int slices = (k1 - k0 + BK - 1) / BK;
+        if (slices <= 0) return;
         SA sa;
         SB sb;
         sa.init(a, a0);
         sb.init(b, b0);
-        if (k0 < k1) {
-            sa.issue(k0, lds);
-            sb.issue(k0, lds + SA::BYTES);
-        }
-        int stage = 0;
-        for (int k = k0; k < k1; k += BK, stage ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            unsigned char* ta = lds + stage * (SA::BYTES + SB::BYTES);
-            unsigned char* tb = ta + SA::BYTES;
-            if (k + BK < k1) {
-                unsigned char* next = lds + (stage ^ 1) * (SA::BYTES + SB::BYTES);
-                sa.issue(k + BK, next);
-                sb.issue(k + BK, next + SA::BYTES);
+        const auto fill = [&](int s) {
+            unsigned char* t = lds + s % STAGES * STAGE;
+            sa.issue(k0 + s * BK, t);
+            sb.issue(k0 + s * BK, t + SA::BYTES);
+        };
+        typename E::frag fa[2][TMI], fb[2][TNI];
+        const auto read = [&](int buf, int s, int step) {
+            const unsigned char* t = lds + s % STAGES * STAGE;
+#pragma unroll
+            for (int i = 0; i < TMI; ++i) {
+                if constexpr (ACOL) fa[buf][i] = SA::T::template col_frag<true>(t, 0, wm / 32 + i, step, lane);
+                else fa[buf][i] = SA::T::row_frag(t, wm + 32 * i + l32, step, half);
             }
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                typename E::frag fa[2], fb[2];
+            for (int j = 0; j < TNI; ++j) {
+                if constexpr (BCOL) fb[buf][j] = SB::T::template col_frag<true>(t + SA::BYTES, 0, wn / 32 + j, step, lane);
+                else fb[buf][j] = SB::T::row_frag(t + SA::BYTES, wn + 32 * j + l32, step, half);
+            }
+        };
+        const auto multiply = [&](int buf) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if constexpr (ACOL) fa[i] = SA::T::template col_frag<true>(ta, 0, wm / 32 + i, s, lane);
-                    else fa[i] = SA::T::row_frag(ta, wm + 32 * i + l32, s, half);
-                    if constexpr (BCOL) fb[i] = SB::T::template col_frag<true>(tb, 0, wn / 32 + i, s, lane);
-                    else fb[i] = SB::T::row_frag(tb, wn + 32 * i + l32, s, half);
+            for (int i = 0; i < TMI; ++i)
+#pragma unroll
+                for (int j = 0; j < TNI; ++j) acc[i][j] = E::mma(fa[buf][i], fb[buf][j], acc[i][j]);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < slices) fill(s);
+        wait_slices(min(STAGES - 2, slices - 1));
+        __builtin_amdgcn_s_barrier();
+        read(0, 0, 0);
+        static_assert(STEPS % 2 == 0, "the operands' two buffers alternate by step");
+        for (int s = 0; s < slices; ++s) {
+            const bool more = s + STAGES - 1 < slices;
+#pragma unroll
+            for (int step = 0; step < STEPS; ++step) {
+                if (step + 1 < STEPS) {
+                    read((step + 1) & 1, s, step + 1);
+                    if (step == 0 && more) fill(s + STAGES - 1);
+                } else if (s + 1 < slices) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    wait_slices(more ? STAGES - 2 : slices - 2 - s);
+                    __builtin_amdgcn_s_barrier();
+                    read(0, s + 1, 0);
                 }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = E::mma(fa[i], fb[j], acc[i][j]);
+                multiply(step & 1);
             }
         }
     }
 };
 
+// Workgroup id -> block of a grid of m x n: consecutive ids go to the 8 XCDs in turn, so each gets a run of blocks of its own, which walks bands of
+// kBand blocks of m and shares their operands in that XCD's L2.
+constexpr int kBand = 8;
+__device__ __forceinline__ void block_of(int id, int m, int n, int& bm, int& bn)
+{
+    const int total = m * n, x = id & 7, q = total >> 3, r = total & 7;
+    const int t = x * q + min(x, r) + (id >> 3);
+    const int band = t / (kBand * n), in_band = min(kBand, m - band * kBand), tb = t - band * kBand * n;
+    bn = tb / in_band;
+    bm = band * kBand + tb % in_band;
+}
+
+// Blocks of a launch: FEW for up to 32 tokens (a stream of weights), MID 128 x 128, BIG 256 x 256 of 8 wavefronts (bfloat16).
+enum { FEW, MID, BIG };
+template <typename E, bool ACOL, bool BCOL, int C>
+struct Pick;
+template <bool A, bool B>
+struct Pick<B16, A, B, FEW> { typedef Product<B16, A, B, 4, 1, 1, 1, 64, 4> P; };
+template <bool A, bool B>
+struct Pick<B16, A, B, MID> { typedef Product<B16, A, B, 2, 2, 2, 2, 32, 4> P; };
+template <bool A, bool B>
+struct Pick<B16, A, B, BIG> { typedef Product<B16, A, B, 2, 4, 4, 2, 32, 4> P; };
+template <bool A, bool B>
+struct Pick<F32, A, B, FEW> { typedef Product<F32, A, B, 4, 1, 1, 1, 32, 4> P; };
+template <bool A, bool B>
+struct Pick<F32, A, B, MID> { typedef Product<F32, A, B, 2, 2, 2, 2, 32, 2> P; };
+
 struct Stat {
     float top, sum;         // sum of exp2(log2e (z - top))
 };
 
-// ---- forward: one 128 x 128 block of z (vocabulary in registers, tokens in lanes) -> a Stat per token and 64 entries of the vocabulary
-template <typename E>
-__global__ __launch_bounds__(256) void vocab_stats_kernel(VocabLoss p, const int32_t* count, const int32_t* index, Stat* stats, float* at_label)
+// ---- forward: a block of z (vocabulary in registers, tokens in lanes) -> a Stat per token and wavefront's range of the vocabulary
+template <typename E, int C>
+__global__ __launch_bounds__((Pick<E, false, false, C>::P::NT)) void vocab_stats_kernel(VocabLoss p, const int32_t* count, const int32_t* index, Stat* stats, float* at_label)
 {
-    using P = Product<E, false, false>;
+    typedef typename Pick<E, false, false, C>::P P;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int n = *count, t0 = blockIdx.x * kTok, v0 = blockIdx.y * kVoc;
-    if (t0 >= n) return;
-    f32x16 acc[2][2];
+    const int n = count ? *count : p.tokens, t_blocks = (n + P::BN - 1) / P::BN, v_blocks = (p.vocab + P::BM - 1) / P::BM;
+    if ((int)blockIdx.x >= t_blocks * v_blocks) return;
+    int bt, bv;
+    block_of(blockIdx.x, t_blocks, v_blocks, bt, bv);
+    const int t0 = bt * P::BN, v0 = bv * P::BM;
+    f32x16 acc[P::tmi][P::tni];
     P::run(acc, Operand{p.w, p.ldw, nullptr, p.vocab, 0}, v0, Operand{p.x, p.ldx, index, n, 0}, t0, 0, p.hidden, lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-    const int vb = v0 + (wave >> 1) * 64, tb = t0 + (wave & 1) * 64;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int vb = v0 + P::wave_m(), tb = t0 + P::wave_n();
     if (vb >= p.vocab) return;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < P::tni; ++j) {
         const int t = tb + j * 32 + l32;
-        const int label = t < n ? p.labels[index[t]] : -1;
+        const int label = t < n ? p.labels[index ? index[t] : t] : -1;
         float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int v = vb + i * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
@@ -189,30 +258,53 @@ __global__ __launch_bounds__(256) void vocab_stats_kernel(VocabLoss p, const int
         top = lane_pair_max<32>(top);
         const float from = top == -INFINITY ? 0.f : top * kLog2e;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -from));
         sum = lane_pair_sum<32>(sum);
-        if (t < n && half == 0) stats[(int64_t)(vb / 64) * p.tokens + t] = Stat{top, sum};
+        if (t < n && half == 0) stats[(int64_t)(vb / (P::tmi * 32)) * p.tokens + t] = Stat{top, sum};
     }
 }
 
-// one wavefront a token: the ranges joined; tokens without a label get zeros
+// the ranges joined: TOK tokens a workgroup, 256 / TOK threads each; tokens without a label get zeros
+template <int TOK>
 __global__ __launch_bounds__(256) void vocab_join_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const Stat* stats, const float* at_label, int ranges)
 {
-    const int t = blockIdx.x * 256 + threadIdx.x;
-    if (t < p.tokens && (uint32_t)p.labels[t] >= (uint32_t)p.vocab) p.loss[t] = p.lse[t] = 0.f;
-    if (t >= *count) return;
+    constexpr int SLICES = 256 / TOK;
+    __shared__ Stat part[SLICES][TOK];
+    const int slice = threadIdx.x / TOK, t = blockIdx.x * TOK + threadIdx.x % TOK;
+    const bool in = t < p.tokens, none = in && (uint32_t)p.labels[t] >= (uint32_t)p.vocab;
+    if (slice == 0 && none) p.loss[t] = p.lse[t] = 0.f;
+    const int n = count ? *count : p.tokens;
+    if ((int)blockIdx.x * TOK >= n) return;
+    const bool mine = t < n && (index || !none);
+    Stat s{-INFINITY, 0.f};
+    for (int r0 = slice; r0 < ranges; r0 += 8 * SLICES) {
+        Stat v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = stats[(int64_t)min(r0 + k * SLICES, ranges - 1) * p.tokens + min(t, n - 1)];
+        float top = s.top;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, v[k].top);
+        const float from = top == -INFINITY ? 0.f : top;
+        s.sum *= __builtin_amdgcn_exp2f((s.top - from) * kLog2e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (r0 + k * SLICES < ranges) s.sum = fmaf(v[k].sum, __builtin_amdgcn_exp2f((v[k].top - from) * kLog2e), s.sum);
+        s.top = top;
+    }
+    part[slice][threadIdx.x % TOK] = s;
+    __syncthreads();
+    if (slice != 0 || !mine) return;
     float top = -INFINITY;
-    for (int r = 0; r < ranges; ++r) top = fmaxf(top, stats[(int64_t)r * p.tokens + t].top);
+#pragma unroll
+    for (int k = 0; k < SLICES; ++k) top = fmaxf(top, part[k][threadIdx.x].top);
     const float from = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int r = 0; r < ranges; ++r) {
-        const Stat s = stats[(int64_t)r * p.tokens + t];
-        sum = fmaf(s.sum, __builtin_amdgcn_exp2f((s.top - from) * kLog2e), sum);
-    }
+#pragma unroll
+    for (int k = 0; k < SLICES; ++k) sum = fmaf(part[k][threadIdx.x].sum, __builtin_amdgcn_exp2f((part[k][threadIdx.x].top - from) * kLog2e), sum);
     const float lse = top + __builtin_amdgcn_logf(sum) * kLn2;
-    const int at = index[t];
+    const int at = index ? index[t] : t;
     p.lse[at] = lse;
     p.loss[at] = lse - at_label[t];
 }
@@ -231,37 +323,40 @@ __global__ __launch_bounds__(256) void labelled_rows_kernel(VocabLoss p, const i
 }
 
 // dz of one piece of the vocabulary [piece0, piece0 + width) (columns beyond the vocabulary: 0), rows beyond the labelled ones up to a whole slice: 0
-template <typename E>
-__global__ __launch_bounds__(256) void vocab_dz_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const typename E::elem* xc, int piece0, int width,
-                                                       typename E::elem* dz)
+template <typename E, int C>
+__global__ __launch_bounds__((Pick<E, false, false, C>::P::NT)) void vocab_dz_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const typename E::elem* xc,
+                                                                                     int piece0, int width, typename E::elem* dz)
 {
-    using P = Product<E, false, false>;
+    typedef typename Pick<E, false, false, C>::P P;
     typedef typename E::elem out4 __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int n = *count, t0 = blockIdx.x * kTok, v0 = piece0 + blockIdx.y * kVoc;
-    if (t0 >= n) return;
-    f32x16 acc[2][2];
-    // (a tile behind the vocabulary, whose columns of dz are zeros, multiplies nothing)
+    const int n = *count, t_blocks = (n + P::BN - 1) / P::BN, v_blocks = width / P::BM;
+    if ((int)blockIdx.x >= t_blocks * v_blocks) return;
+    int bt, bv;
+    block_of(blockIdx.x, t_blocks, v_blocks, bt, bv);
+    const int t0 = bt * P::BN, v0 = piece0 + bv * P::BM;
+    f32x16 acc[P::tmi][P::tni];
+    // (a block behind the vocabulary, whose columns of dz are zeros, multiplies nothing)
     P::run(acc, Operand{p.w, p.ldw, nullptr, p.vocab, 0}, v0, Operand{xc, p.hidden, nullptr, n, 0}, t0, 0, v0 < p.vocab ? p.hidden : 0, lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-    const int vb = v0 + (wave >> 1) * 64, tb = t0 + (wave & 1) * 64;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int vb = v0 + P::wave_m(), tb = t0 + P::wave_n();
     const int n_pad = (n + 63) & ~63;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < P::tni; ++j) {
         const int t = tb + j * 32 + l32;
         if (t >= n_pad) continue;
         const bool real = t < n;
         const int at = real ? index[t] : 0, label = real ? p.labels[at] : -1;
         const float lse = real ? p.lse[at] * kLog2e : 0.f, g = real ? p.weight[at] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int v = vb + i * 32 + 8 * q + 4 * half;
                 out4 o;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float w = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], kLog2e, -lse)) - (v + e == label ? 1.f : 0.f);
+                    const float w = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], kLog2e, -lse)) - (v + e == label ? 1.f : 0.f);
                     o[e] = (typename E::elem)(real && v + e < p.vocab ? w * g : 0.f);
                 }
                 *reinterpret_cast<out4*>(dz + (int64_t)t * width + v - piece0) = o;
@@ -269,30 +364,45 @@ __global__ __launch_bounds__(256) void vocab_dz_kernel(VocabLoss p, const int32_
     }
 }
 
-// dx += dz W over one piece, float32 sums in memory; the piece is cut into `splits` ranges with sums of their own
-template <typename E>
-__global__ __launch_bounds__(256) void vocab_dx_kernel(VocabLoss p, const int32_t* count, const typename E::elem* dz, int piece0, int width, int splits, float* part)
+// How many ranges of the vocabulary dx is summed in: as many as fill the chip with the blocks that n labelled tokens have.
+struct Ranges {
+    int most, blocks;       // most ranges; workgroups wanted
+    __host__ __device__ int of(int64_t tiles) const
+    {
+        const int64_t r = blocks / (tiles > 0 ? tiles : 1);
+        return (int)(r < 1 ? 1 : r < most ? r : most);
+    }
+};
+
+// dx += dz W over one piece, float32 sums in memory, one per range
+template <typename E, int C>
+__global__ __launch_bounds__((Pick<E, true, false, C>::P::NT)) void vocab_dx_kernel(VocabLoss p, const int32_t* count, const typename E::elem* dz, int piece0, int width,
+                                                                                    Ranges ranges, float* part)
 {
-    using P = Product<E, true, false>;
+    typedef typename Pick<E, true, false, C>::P P;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int n = *count, t0 = blockIdx.x * 128, h0 = blockIdx.y * 128, split = blockIdx.z;
-    if (t0 >= n) return;
-    const int slices = width / P::BK, k0 = (int)((int64_t)slices * split / splits) * P::BK, k1 = (int)((int64_t)slices * (split + 1) / splits) * P::BK;
-    f32x16 acc[2][2];
+    const int n = *count, t_blocks = (n + P::BN - 1) / P::BN, h_blocks = (p.hidden + P::BM - 1) / P::BM, tiles = t_blocks * h_blocks, split_n = ranges.of(tiles);
+    if ((int)blockIdx.x >= tiles * split_n) return;
+    // (an XCD's workgroups share ranges, whose part of W and dz its L2 then holds)
+    int bt, split;
+    block_of(blockIdx.x, tiles, split_n, bt, split);
+    const int t0 = bt / h_blocks * P::BN, h0 = bt % h_blocks * P::BM;
+    const int slices = width / P::kBK, k0 = (int)((int64_t)slices * split / split_n) * P::kBK, k1 = (int)((int64_t)slices * (split + 1) / split_n) * P::kBK;
+    f32x16 acc[P::tmi][P::tni];
     const auto* w = static_cast<const typename E::elem*>(p.w) + (int64_t)piece0 * p.ldw;
     P::run(acc, Operand{w, p.ldw, nullptr, p.hidden, p.vocab - piece0}, h0, Operand{dz, width, nullptr, n, 0}, t0, k0, k1, lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int t = t0 + (wave & 1) * 64 + j * 32 + l32;
+    for (int j = 0; j < P::tni; ++j) {
+        const int t = t0 + P::wave_n() + j * 32 + l32;
         if (t >= n) continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int h = h0 + (wave >> 1) * 64 + i * 32 + 8 * q + 4 * half;
+                const int h = h0 + P::wave_m() + i * 32 + 8 * q + 4 * half;
                 if (h >= p.hidden) continue;
-                f32x4* at = reinterpret_cast<f32x4*>(part + ((int64_t)split * p.tokens + t) * p.hidden + h);
+                f32x4* at = reinterpret_cast<f32x4*>(part + ((int64_t)split * n + t) * p.hidden + h);
                 f32x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
@@ -303,25 +413,29 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(VocabLoss p, const int32_
 }
 
 // dW of one piece: the sum over the labelled tokens
-template <typename E, typename Out>
-__global__ __launch_bounds__(256) void vocab_dw_kernel(VocabLoss p, const int32_t* count, const typename E::elem* dz, const typename E::elem* xc, int piece0, int width)
+template <typename E, typename Out, int C>
+__global__ __launch_bounds__((Pick<E, true, true, C>::P::NT)) void vocab_dw_kernel(VocabLoss p, const int32_t* count, const typename E::elem* dz,
+                                                                                   const typename E::elem* xc, int piece0, int width)
 {
-    using P = Product<E, true, true>;
+    typedef typename Pick<E, true, true, C>::P P;
     typedef Out out4 __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int n = *count, h0 = blockIdx.x * 128, v0 = blockIdx.y * 128;
-    f32x16 acc[2][2];
-    P::run(acc, Operand{xc, p.hidden, nullptr, p.hidden, n}, h0, Operand{dz, width, nullptr, width, (n + 63) & ~63}, v0, 0, (n + P::BK - 1) / P::BK * P::BK, lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int n = *count, h_blocks = (p.hidden + P::BM - 1) / P::BM, v_blocks = (width + P::BN - 1) / P::BN;
+    int bh, bv;
+    block_of(blockIdx.x, h_blocks, v_blocks, bh, bv);
+    const int h0 = bh * P::BM, v0 = bv * P::BN;
+    f32x16 acc[P::tmi][P::tni];
+    P::run(acc, Operand{xc, p.hidden, nullptr, p.hidden, n}, h0, Operand{dz, width, nullptr, width, (n + 63) & ~63}, v0, 0, n, lds);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int v = piece0 + v0 + (wave & 1) * 64 + j * 32 + l32;
-        if (v >= p.vocab) continue;
+    for (int j = 0; j < P::tni; ++j) {
+        const int v = piece0 + v0 + P::wave_n() + j * 32 + l32;
+        if (v >= min(p.vocab, piece0 + width)) continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int h = h0 + (wave >> 1) * 64 + i * 32 + 8 * q + 4 * half;
+                const int h = h0 + P::wave_m() + i * 32 + 8 * q + 4 * half;
                 if (h >= p.hidden) continue;
                 out4 o;
 #pragma unroll
@@ -333,9 +447,9 @@ __global__ __launch_bounds__(256) void vocab_dw_kernel(VocabLoss p, const int32_
 
 // dx: the ranges' sums put together and rounded, in the tokens' places; zeros for tokens without a label
 template <typename E>
-__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const float* part, int splits)
+__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const float* part, Ranges ranges, int bm, int bn)
 {
-    const int per = p.hidden / 4;
+    const int per = p.hidden / 4, n = *count;
     typedef typename E::elem out4 __attribute__((ext_vector_type(4)));
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int row = (int)(at / per), c = (int)(at - (int64_t)row * per) * 4;
@@ -347,9 +461,10 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const i
         for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)0.f;
         *reinterpret_cast<out4*>(dx + (int64_t)row * p.hidden + c) = o;
     }
-    if (row >= *count) return;
+    if (row >= n) return;
+    const int splits = ranges.of((int64_t)((n + bn - 1) / bn) * ((p.hidden + bm - 1) / bm));
     f32x4 v{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(part + ((int64_t)s * p.tokens + row) * p.hidden + c);
+    for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(part + ((int64_t)s * n + row) * p.hidden + c);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)v[e];
     *reinterpret_cast<out4*>(dx + (int64_t)index[row] * p.hidden + c) = o;
@@ -357,54 +472,79 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const i
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// The kind of blocks, by the bound on the tokens: BIG where that makes enough of them for the chip.
+template <typename E>
+int blocks_for(int tokens, int other)
+{
+    if (tokens <= 32) return FEW;
+    if (E::SIZE == 2 && (int64_t)((tokens + 255) / 256) * ((other + 255) / 256) >= 256) return BIG;
+    return MID;
+}
+template <typename E, typename F>
+hipError_t with_blocks(int kind, F&& f)
+{
+    if (kind == FEW) return f(std::integral_constant<int, FEW>());
+    if constexpr (E::SIZE == 2) {
+        if (kind == BIG) return f(std::integral_constant<int, BIG>());
+    }
+    return f(std::integral_constant<int, MID>());
+}
+int range_of(int kind) { return kind == FEW ? 32 : kind == MID ? 64 : 128; }        // vocabulary entries of a Stat
+
 struct Plan {
-    int piece, splits;
+    int piece;
+    Ranges ranges;
     size_t index, xc, dz, part, bytes;
 };
-Plan grad_plan(int f32, int tokens, int hidden, int vocab)
+template <typename E>
+Plan grad_plan(int tokens, int hidden, int vocab)
 {
-    const size_t es = f32 ? 4 : 2;
-    const size_t rows = (size_t)(tokens + 127) / 128 * 128;
+    const size_t es = E::SIZE, rows = (size_t)(tokens + 63) / 64 * 64;
     Plan p;
-    // pieces whose dz (at most 128 MB) stays in the last-level cache until both products have read it
-    const size_t fit = (size_t)(128u << 20) / (rows * es) / kPieceGrain * kPieceGrain;
-    const size_t whole = ((size_t)vocab + kPieceGrain - 1) / kPieceGrain * kPieceGrain;
+    // pieces of the vocabulary: dz of at most 256 MB, the size of the last-level cache
+    const size_t fit = (size_t)(256u << 20) / (rows * es) / 256 * 256, whole = ((size_t)vocab + 255) / 256 * 256;
     p.piece = (int)std::min(whole, std::max<size_t>(fit, 1024));
-    // enough workgroups for dx, whose tiles are few
-    const long tiles = (long)(rows / 128) * ((hidden + 127) / 128);
-    p.splits = (int)std::max<long>(1, std::min<long>({8, 512 / tiles, p.piece / 512}));
+    const int kind = blocks_for<E>(tokens, vocab), bm = kind == BIG ? 256 : 128, bn = kind == BIG ? 256 : kind == MID ? 128 : 32, h_blocks = (hidden + bm - 1) / bm;
+    p.ranges = Ranges{std::max(1, std::min(64, p.piece / 256)), kind == BIG ? 256 : 512};
+    const size_t part_rows = std::max<size_t>(tokens, std::min<size_t>((size_t)p.ranges.most * tokens, (size_t)p.ranges.blocks * bn / h_blocks));
     p.index = 256;
     p.xc = p.index + up256((size_t)tokens * 4);
     p.dz = p.xc + up256(rows * hidden * es);
     p.part = p.dz + up256(rows * p.piece * es);
-    p.bytes = p.part + up256((size_t)p.splits * tokens * hidden * 4);
+    p.bytes = p.part + up256(part_rows * hidden * 4);
     return p;
-}
-
-template <typename K>
-hipError_t with_lds(K* kernel, int bytes, std::atomic<uint64_t>& done)
-{
-    return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, done);
 }
 
 template <typename E>
 hipError_t forward_of(const VocabLoss& p, hipStream_t stream)
 {
-    static std::atomic<uint64_t> done{0};
-    constexpr int lds = Product<E, false, false>::LDS;
-    hipError_t e = with_lds(vocab_stats_kernel<E>, lds, done);
-    if (e != hipSuccess) return e;
+    const int kind = blocks_for<E>(p.tokens, p.vocab), ranges = (p.vocab + range_of(kind) - 1) / range_of(kind);
     unsigned char* ws = static_cast<unsigned char*>(p.work);
-    const int ranges = (p.vocab + 63) / 64;
+    const size_t list = up256((size_t)p.tokens * 4);
     int32_t* count = reinterpret_cast<int32_t*>(ws);
     int32_t* index = reinterpret_cast<int32_t*>(ws + 256);
-    float* at_label = reinterpret_cast<float*>(ws + 256 + up256((size_t)p.tokens * 4));
-    Stat* stats = reinterpret_cast<Stat*>(ws + 256 + 2 * up256((size_t)p.tokens * 4));
-    label_index_kernel<<<1, 1024, 0, stream>>>(p.labels, p.tokens, p.vocab, count, index);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    vocab_stats_kernel<E><<<dim3((p.tokens + kTok - 1) / kTok, (p.vocab + kVoc - 1) / kVoc), 256, lds, stream>>>(p, count, index, stats, at_label);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    vocab_join_kernel<<<(p.tokens + 255) / 256, 256, 0, stream>>>(p, count, index, stats, at_label, ranges);
+    float* at_label = reinterpret_cast<float*>(ws + 256 + list);
+    Stat* stats = reinterpret_cast<Stat*>(ws + 256 + 2 * list);
+    hipError_t e;
+    if (kind == FEW) count = index = nullptr;           // a block takes all the tokens: nothing to gain by listing the labelled ones
+    else {
+        label_index_kernel<<<1, 1024, 0, stream>>>(p.labels, p.tokens, p.vocab, count, index);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    e = with_blocks<E>(kind, [&](auto c) {
+        typedef typename Pick<E, false, false, c.value>::P P;
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_stats_kernel<E, c.value>), P::LDS, done);
+        if (e != hipSuccess) return e;
+        const int64_t grid = (int64_t)((p.tokens + P::BN - 1) / P::BN) * ((p.vocab + P::BM - 1) / P::BM);
+        if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+        vocab_stats_kernel<E, c.value><<<(unsigned)grid, P::NT, P::LDS, stream>>>(p, count, index, stats, at_label);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    // few tokens: more threads each
+    if (p.tokens <= 256) vocab_join_kernel<4><<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, count, index, stats, at_label, ranges);
+    else vocab_join_kernel<16><<<(p.tokens + 15) / 16, 256, 0, stream>>>(p, count, index, stats, at_label, ranges);
     return hipGetLastError();
 }
 
@@ -412,42 +552,60 @@ template <typename E>
 hipError_t gradient_of(const VocabLoss& p, hipStream_t stream)
 {
     typedef typename E::elem elem;
-    static std::atomic<uint64_t> done_dz{0}, done_dx{0}, done_dw{0}, done_dwf{0};
-    constexpr int lds_dz = Product<E, false, false>::LDS, lds_dx = Product<E, true, false>::LDS, lds_dw = Product<E, true, true>::LDS;
     hipError_t e;
-    if ((e = with_lds(vocab_dz_kernel<E>, lds_dz, done_dz)) != hipSuccess || (e = with_lds(vocab_dx_kernel<E>, lds_dx, done_dx)) != hipSuccess ||
-        (e = with_lds(vocab_dw_kernel<E, elem>, lds_dw, done_dw)) != hipSuccess || (e = with_lds(vocab_dw_kernel<E, float>, lds_dw, done_dwf)) != hipSuccess)
-        return e;
-    const Plan pl = grad_plan(E::SIZE == 4, p.tokens, p.hidden, p.vocab);
+    const Plan pl = grad_plan<E>(p.tokens, p.hidden, p.vocab);
     unsigned char* ws = static_cast<unsigned char*>(p.work);
     int32_t* count = reinterpret_cast<int32_t*>(ws);
     int32_t* index = reinterpret_cast<int32_t*>(ws + pl.index);
     elem* xc = reinterpret_cast<elem*>(ws + pl.xc);
     elem* dz = reinterpret_cast<elem*>(ws + pl.dz);
     float* part = reinterpret_cast<float*>(ws + pl.part);
-    const unsigned t_tiles = (p.tokens + 127) / 128, h_tiles = (p.hidden + 127) / 128;
     label_index_kernel<<<1, 1024, 0, stream>>>(p.labels, p.tokens, p.vocab, count, index);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     labelled_rows_kernel<E><<<(unsigned)(((int64_t)p.tokens * (p.hidden / E::EPC) + 255) / 256), 256, 0, stream>>>(p, count, index, xc);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    for (int v0 = 0; v0 < p.vocab; v0 += pl.piece) {
-        const int width = std::min(pl.piece, (p.vocab - v0 + kPieceGrain - 1) / kPieceGrain * kPieceGrain);
-        vocab_dz_kernel<E><<<dim3(t_tiles, width / kVoc), 256, lds_dz, stream>>>(p, count, index, xc, v0, width, dz);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        vocab_dx_kernel<E><<<dim3(t_tiles, h_tiles, pl.splits), 256, lds_dx, stream>>>(p, count, dz, v0, width, pl.splits, part);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        if (p.dw_f32) vocab_dw_kernel<E, float><<<dim3(h_tiles, width / 128), 256, lds_dw, stream>>>(p, count, dz, xc, v0, width);
-        else vocab_dw_kernel<E, elem><<<dim3(h_tiles, width / 128), 256, lds_dw, stream>>>(p, count, dz, xc, v0, width);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    vocab_dx_rows_kernel<E><<<(unsigned)(((int64_t)p.tokens * (p.hidden / 4) + 255) / 256), 256, 0, stream>>>(p, count, index, part, pl.splits);
-    return hipGetLastError();
+    return with_blocks<E>(blocks_for<E>(p.tokens, p.vocab), [&](auto c) {
+        constexpr int C = c.value, CW = C == FEW ? MID : C;      // (dW has no tokens among its blocks)
+        typedef typename Pick<E, false, false, C>::P PZ;
+        typedef typename Pick<E, true, false, C>::P PX;
+        typedef typename Pick<E, true, true, CW>::P PW;
+        static std::atomic<uint64_t> done_z{0}, done_x{0}, done_w{0}, done_wf{0};
+        hipError_t e;
+        if ((e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_dz_kernel<E, C>), PZ::LDS, done_z)) != hipSuccess ||
+            (e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_dx_kernel<E, C>), PX::LDS, done_x)) != hipSuccess ||
+            (e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_dw_kernel<E, elem, CW>), PW::LDS, done_w)) != hipSuccess ||
+            (e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_dw_kernel<E, float, CW>), PW::LDS, done_wf)) != hipSuccess)
+            return e;
+        for (int v0 = 0; v0 < p.vocab; v0 += pl.piece) {
+            const int width = std::min(pl.piece, (p.vocab - v0 + 255) / 256 * 256);
+            const int64_t grid_z = (int64_t)((p.tokens + PZ::BN - 1) / PZ::BN) * (width / PZ::BM);
+            const int64_t tiles_x = (int64_t)((p.tokens + PX::BN - 1) / PX::BN) * ((p.hidden + PX::BM - 1) / PX::BM), grid_x = std::max<int64_t>(tiles_x, pl.ranges.blocks);
+            const int64_t grid_w = (int64_t)((p.hidden + PW::BM - 1) / PW::BM) * ((width + PW::BN - 1) / PW::BN);
+            if (std::max({grid_z, grid_x, grid_w}) > 0x7FFFFFFF) return hipErrorInvalidValue;
+            vocab_dz_kernel<E, C><<<(unsigned)grid_z, PZ::NT, PZ::LDS, stream>>>(p, count, index, xc, v0, width, dz);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            vocab_dx_kernel<E, C><<<(unsigned)grid_x, PX::NT, PX::LDS, stream>>>(p, count, dz, v0, width, pl.ranges, part);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            if (p.dw_f32) vocab_dw_kernel<E, float, CW><<<(unsigned)grid_w, PW::NT, PW::LDS, stream>>>(p, count, dz, xc, v0, width);
+            else vocab_dw_kernel<E, elem, CW><<<(unsigned)grid_w, PW::NT, PW::LDS, stream>>>(p, count, dz, xc, v0, width);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+        vocab_dx_rows_kernel<E><<<(unsigned)(((int64_t)p.tokens * (p.hidden / 4) + 255) / 256), 256, 0, stream>>>(p, count, index, part, pl.ranges, PX::BM, PX::BN);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
 
-size_t vocab_loss_work(int tokens, int vocab) { return 256 + 2 * up256((size_t)tokens * 4) + (size_t)((vocab + 63) / 64) * tokens * sizeof(Stat); }
-size_t vocab_loss_grad_work(int f32, int tokens, int hidden, int vocab) { return grad_plan(f32, tokens, hidden, vocab).bytes; }
+size_t vocab_loss_work(int tokens, int vocab)
+{
+    const int range = range_of(tokens <= 32 ? FEW : MID);
+    return 256 + 2 * up256((size_t)tokens * 4) + (size_t)((vocab + range - 1) / range) * tokens * sizeof(Stat);
+}
+size_t vocab_loss_grad_work(int f32, int tokens, int hidden, int vocab)
+{
+    return f32 ? grad_plan<F32>(tokens, hidden, vocab).bytes : grad_plan<B16>(tokens, hidden, vocab).bytes;
+}
 
 hipError_t launch_vocab_loss(const VocabLoss& p, int f32, hipStream_t stream) { return f32 ? forward_of<F32>(p, stream) : forward_of<B16>(p, stream); }
 hipError_t launch_vocab_loss_grad(const VocabLoss& p, int f32, hipStream_t stream) { return f32 ? gradient_of<F32>(p, stream) : gradient_of<B16>(p, stream); }
