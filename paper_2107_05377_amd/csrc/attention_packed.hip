@@ -188,7 +188,7 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
 // rows row0 .. row0 + ROWS - 1 (none beyond `last`, whose copy stands in) of a matrix into an LDS tile, 16 bytes a lane straight from memory.
 // Columns beyond the head's width hold copies of the first ones: they meet zeros, or results that nobody stores.
 template <typename E, int DP, int ROWS, int NW, bool GROUPED>
-__device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_stride, int64_t head_stride, int group, int row0, int last, int d, unsigned char* t)
+__device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_stride, int64_t head_stride, int group, int row0, int last, int d, uint32_t t)
 {
     using T = Tile<E, DP>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -206,7 +206,7 @@ __device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_
             const int tok = r / group;
             at = base + tok * row_stride + (r - tok * group) * head_stride;
         } else at = base + r * row_stride;
-        __builtin_amdgcn_global_load_lds((gptr_t)(at + chunk * E::EPC), (lptr_t)(t + blk * 1024), 16, 0, 0);
+        load_to_lds(at + chunk * E::EPC, t + blk * 1024);
     }
 }
 
@@ -226,6 +226,15 @@ __device__ __forceinline__ void load_row(typename E::frag (&f)[DP / E::KS], cons
         for (int j = 0; j < E::EPC; ++j) f[ks][j] = (typename E::elem)0.f;
         if (c < d) f[ks] = *reinterpret_cast<const typename E::frag*>(row + c);
     }
+}
+
+// Registers loaded from memory are used here: the compiler's wait for them stands here too, and not in the loop behind, where it would be one for the
+// tiles under way.
+template <typename F, int N>
+__device__ __forceinline__ void loaded(const F (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" ::"v"(f[i]));
 }
 
 template <typename E, int DP>
@@ -254,6 +263,7 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
     typedef typename E::elem elem;
     constexpr int BM = NW * 32, TK = kTileKeys, BYTES = TK * T::ROWB;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of keys and values
+    const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
     if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
@@ -281,15 +291,16 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
     float ref = -INFINITY, sum = 0.f;       // weights are exp2(c (score - ref))
 
     if (n_tiles > 0) {
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds + BYTES);
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds0);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds0 + BYTES);
     }
+    loaded(qf);
     for (int kt = 0; kt < n_tiles; ++kt) {
         loads_landed();
         const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
         const unsigned char* tv = tk + BYTES;
         if (kt + 1 < n_tiles) {
-            unsigned char* next = lds + ((kt + 1) & 1) * 2 * BYTES;
+            const uint32_t next = lds0 + ((kt + 1) & 1) * 2 * BYTES;
             stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
             stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
         }
@@ -360,15 +371,15 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
     }
 }
 
-// delta = dctx . ctx per (head, query): one wavefront per 8 rows, 8 lanes a row
+// What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and delta = dctx . ctx.  8 lanes a row.
 template <typename E>
-__global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* delta)
+__global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* stat)
 {
     typedef typename E::elem elem;
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3, all = (int64_t)p.total_q * p.heads;
     const int part = threadIdx.x & 7;
-    if (at >= (int64_t)p.total_q * p.heads) return;
-    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads);
+    if (at >= all) return;
+    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads), group = p.heads / p.kv_heads, kvh = head / group;
     const elem* o = static_cast<const elem*>(p.ctx) + row * p.o_row + head * p.o_head;
     const elem* g = static_cast<const elem*>(p.dctx) + row * p.g_row + head * p.g_head;
     float sum = 0.f;
@@ -380,17 +391,20 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* 
     sum += __shfl_xor(sum, 1);
     sum += __shfl_xor(sum, 2);
     sum += __shfl_xor(sum, 4);
-    if (part == 0) delta[(int64_t)head * p.total_q + row] = sum;
+    const int64_t to = (int64_t)kvh * p.total_q * group + (int64_t)row * group + head - kvh * group;
+    if (part == 0) stat[to] = p.lse_in[(int64_t)head * p.total_q + row] * kLog2e;
+    if (part == 1) stat[all + to] = sum;
 }
 
 // dq: rows fixed, keys pass by
 template <typename E, int DP, int NW>
-__global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const float* delta)
+__global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const float* stat)
 {
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
     constexpr int BM = NW * 32, TK = 32, BYTES = TK * T::ROWB;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
     if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
@@ -410,7 +424,8 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
     load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
     load_row<E, DP>(gf, static_cast<const elem*>(p.dctx) + (int64_t)(s.q0 + tok) * p.g_row + head * p.g_head, p.d, half);
     const float c = p.scale * kLog2e;
-    const float lse = p.lse_in[(int64_t)head * p.total_q + s.q0 + tok] * kLog2e, dl = delta[(int64_t)head * p.total_q + s.q0 + tok];
+    const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group + my_row;
+    const float lse = my_stat[0], dl = my_stat[(int64_t)p.total_q * p.heads];
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -418,15 +433,18 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
     if (n_tiles > 0) {
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds + BYTES);
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds0);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds0 + BYTES);
     }
+    loaded(qf);
+    loaded(gf);
+    asm volatile("" ::"v"(lse), "v"(dl));
     for (int kt = 0; kt < n_tiles; ++kt) {
         loads_landed();
         const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
         const unsigned char* tv = tk + BYTES;
         if (kt + 1 < n_tiles) {
-            unsigned char* next = lds + ((kt + 1) & 1) * 2 * BYTES;
+            const uint32_t next = lds0 + ((kt + 1) & 1) * 2 * BYTES;
             stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
             stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
         }
@@ -449,8 +467,11 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
-            sc[i] = (seen >> i) & 1 ? w : 0.f;
+            sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
+        }
+        if (cut) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = (seen >> i) & 1 ? sc[i] : 0.f;
         }
         add_product<E, DP, true>(acc, tk, 0, sc, cut, seen, lane);
     }
@@ -459,18 +480,19 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
 }
 
 // dk, dv: keys fixed, the rows of all heads of the group pass by
-template <typename E, int DP, int NW>
-__global__ __launch_bounds__(NW * 64) void packed_dkv_kernel(PackedAttn p, const float* delta)
+template <typename E, int DP, int NW, int TQ>
+__global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
 {
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
-    constexpr int BN = NW * 32, TQ = 32, BYTES = TQ * T::ROWB;
+    constexpr int BN = NW * 32, BYTES = TQ * T::ROWB;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of rows of q and dctx; their statistics
     struct RowInfo {
         float lse[TQ], delta[TQ];
         int limit[TQ];
     };
     RowInfo* const info = reinterpret_cast<RowInfo*>(lds + 4 * BYTES);
+    const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
     if (!find_tile(p, blockIdx.x, 1, BN, true, s)) return;
@@ -496,17 +518,17 @@ __global__ __launch_bounds__(NW * 64) void packed_dkv_kernel(PackedAttn p, const
 #pragma unroll
         for (int i = 0; i < 16; ++i) ak[db][i] = av[db][i] = 0.f;
 
+    const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group;
     float r_lse = 0.f, r_delta = 0.f;
     int r_limit = -1;
-    const auto fetch = [&](int rt, unsigned char* to) {
+    const auto fetch = [&](int rt, uint32_t to) {
         stage<E, DP, TQ, NW, true>(Q, p.q_row, p.q_head, group, rt * TQ, rows - 1, p.d, to);
         stage<E, DP, TQ, NW, true>(G, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
         if (threadIdx.x < TQ) {
-            const int r = rt * TQ + threadIdx.x, rr = min(r, rows - 1), t = rr / group;
-            const int64_t at = (int64_t)(kvh * group + rr - t * group) * p.total_q + s.q0 + t;
-            r_lse = p.lse_in[at] * kLog2e;
-            r_delta = delta[at];
-            r_limit = r < rows ? min(t + shift, s.lk - 1) : -1;
+            const int r = rt * TQ + threadIdx.x, rr = min(r, rows - 1);
+            r_lse = my_stat[rr];
+            r_delta = my_stat[rr + (int64_t)p.total_q * p.heads];
+            r_limit = r < rows ? min(rr / group + shift, s.lk - 1) : -1;
         }
     };
     const auto keep = [&](RowInfo& i) {
@@ -516,8 +538,10 @@ __global__ __launch_bounds__(NW * 64) void packed_dkv_kernel(PackedAttn p, const
             i.limit[threadIdx.x] = r_limit;
         }
     };
+    loaded(kf);
+    loaded(vf);
     if (rt0 < n_tiles) {
-        fetch(rt0, lds);
+        fetch(rt0, lds0);
         keep(info[0]);
     }
     for (int rt = rt0; rt < n_tiles; ++rt) {
@@ -527,41 +551,49 @@ __global__ __launch_bounds__(NW * 64) void packed_dkv_kernel(PackedAttn p, const
         const unsigned char* tg = tq + BYTES;
         const RowInfo& in = info[at];
         const bool more = rt + 1 < n_tiles;
-        if (more) fetch(rt + 1, lds + (at ^ 1) * 2 * BYTES);
-        // the tile's last row sees most
-        const int last_limit = min(min((rt * TQ + TQ - 1), rows - 1) / group + shift, s.lk - 1), first_limit = min(rt * TQ / group + shift, s.lk - 1);
-        if (wave_first <= last_limit) {
+        if (more) fetch(rt + 1, lds0 + (at ^ 1) * 2 * BYTES);
+#pragma unroll
+        for (int u = 0; u < TQ / 32; ++u) {
+            const int b0 = rt * TQ + u * 32;
+            // the block's last row sees most
+            const int last_limit = min(min(b0 + 31, rows - 1) / group + shift, s.lk - 1), first_limit = min(b0 / group + shift, s.lk - 1);
+            if (b0 >= rows || wave_first > last_limit) continue;
             f32x16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < DP / E::KS; ++ks) {
-                sc = E::mma(T::row_frag(tq, l32, ks, half), kf[ks], sc);
-                dp = E::mma(T::row_frag(tg, l32, ks, half), vf[ks], dp);
+                sc = E::mma(T::row_frag(tq, u * 32 + l32, ks, half), kf[ks], sc);
+                dp = E::mma(T::row_frag(tg, u * 32 + l32, ks, half), vf[ks], dp);
             }
-            const bool cut = wave_last > first_limit || rt * TQ + TQ > rows;
+            const bool cut = wave_last > first_limit || b0 + 32 > rows;
             uint32_t seen = 0xFFFFu;
             if (cut) {
                 seen = 0;
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
+                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[u * 32 + 8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[8 * g + 4 * half]);
+                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[u * 32 + 8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[u * 32 + 8 * g + 4 * half]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * g + j;
-                    const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -l[j]));
-                    const float ds = w * (dp[i] - dl[j]);
-                    sc[i] = (seen >> i) & 1 ? w : 0.f;
-                    dp[i] = (seen >> i) & 1 ? ds : 0.f;
+                    sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -l[j]));
+                    dp[i] = sc[i] * (dp[i] - dl[j]);
                 }
             }
-            add_product<E, DP, false>(av, tg, 0, sc, cut, seen, lane);
-            add_product<E, DP, true>(ak, tq, 0, dp, cut, seen, lane);
+            if (cut) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sc[i] = (seen >> i) & 1 ? sc[i] : 0.f;
+                    dp[i] = (seen >> i) & 1 ? dp[i] : 0.f;
+                }
+            }
+            add_product<E, DP, false>(av, tg, u * 32, sc, cut, seen, lane);
+            add_product<E, DP, true>(ak, tq, u * 32, dp, cut, seen, lane);
         }
         if (more) keep(info[at ^ 1]);
     }
@@ -589,28 +621,29 @@ hipError_t gradient_with(const PackedAttn& p, hipStream_t stream)
 {
     constexpr int NW = 4;
     static std::atomic<uint64_t> done_q{0}, done_k{0};
-    const int bytes = 4 * 32 * Tile<E, DP>::ROWB, bytes_k = bytes + 2 * 32 * 12;
+    constexpr int TQ = E::SIZE == 2 && DP == 64 ? 64 : 32;
+    const int bytes = 4 * 32 * Tile<E, DP>::ROWB, bytes_k = 4 * TQ * Tile<E, DP>::ROWB + 2 * TQ * 12;
     hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, NW>), bytes, done_q);
     if (e != hipSuccess) return e;
-    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, NW>), bytes_k, done_k);
+    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, NW, TQ>), bytes_k, done_k);
     if (e != hipSuccess) return e;
-    float* delta = static_cast<float*>(p.work);
+    float* stat = static_cast<float*>(p.work);
     const int64_t n = (int64_t)p.total_q * p.heads;
     const int64_t tiles_q = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
     const int64_t tiles_k = ((int64_t)p.total_k + NW * 32 - 1) / (NW * 32) + p.n_seqs;
     if (tiles_q > 0x7FFFFFFF || tiles_k > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
-    packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, delta);
+    packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dkv_kernel<E, DP, NW><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), NW * 64, bytes_k, stream>>>(p, delta);
+    packed_dkv_kernel<E, DP, NW, TQ><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), NW * 64, bytes_k, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dq_kernel<E, DP, NW><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p, delta);
+    packed_dq_kernel<E, DP, NW><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p, stat);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t packed_attention_work(int, int, int, int, int, int, int) { return 0; }
-size_t packed_attention_grad_work(int total_q, int heads) { return (size_t)total_q * heads * 4; }
+size_t packed_attention_grad_work(int total_q, int heads) { return (size_t)total_q * heads * 8; }
 
 hipError_t launch_packed_attention(const PackedAttn& p, int f32, hipStream_t stream)
 {

@@ -12,6 +12,19 @@ typedef __attribute__((address_space(3))) s16x4* l16x4_t;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+__device__ __forceinline__ uint32_t lds_address(const unsigned char* p) { return (uint32_t)(uintptr_t)(lptr_t)p; }
+
+// 16 bytes a lane straight from memory to LDS, lane l's at address `to` + 16 l (`to` the same in all lanes).  As assembly, because the compiler would make every
+// transposing LDS read wait for all such loads under way, the next tiles' among them; the waits are the callers' (s_waitcnt vmcnt, then a barrier), and
+// there is no result in a register that could be used too early.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"        // (that m0 is a reserved register: it is told that this changes it)
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0");
+}
+#pragma clang diagnostic pop
+
 // ---- element types: what 16 bytes of a row mean to the matrix instructions
 struct B16 {
     typedef __bf16 elem;

@@ -85,7 +85,7 @@ struct Stager {
             }
         }
     }
-    __device__ __forceinline__ void issue(int k0, unsigned char* t) const
+    __device__ __forceinline__ void issue(int k0, uint32_t t) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
@@ -93,7 +93,7 @@ struct Stager {
             const typename E::elem* p;
             if constexpr (COLS) p = at[i] + (int64_t)min(k0 + row[i], k_n - 1) * ld;
             else p = at[i] + k0;
-            __builtin_amdgcn_global_load_lds((gptr_t)p, (lptr_t)(t + (wave + i * NW) * 1024), 16, 0, 0);
+            load_to_lds(p, t + (wave + i * NW) * 1024);
         }
     }
 };
@@ -144,7 +144,7 @@ struct Product {
         sa.init(a, a0);
         sb.init(b, b0);
         const auto fill = [&](int s) {
-            unsigned char* t = lds + s % STAGES * STAGE;
+            const uint32_t t = lds_address(lds) + s % STAGES * STAGE;
             sa.issue(k0 + s * BK, t);
             sb.issue(k0 + s * BK, t + SA::BYTES);
         };
@@ -175,22 +175,52 @@ struct Product {
         __builtin_amdgcn_s_barrier();
         read(0, 0, 0);
         static_assert(STEPS % 2 == 0, "the operands' two buffers alternate by step");
-        for (int s = 0; s < slices; ++s) {
-            const bool more = s + STAGES - 1 < slices;
+        // slices whose refill exists: no branch inside, which would cut the reads off from the matrix instructions that cover them
+        int s = 0;
+        for (; s + STAGES - 1 < slices; ++s) {
 #pragma unroll
             for (int step = 0; step < STEPS; ++step) {
                 if (step + 1 < STEPS) {
                     read((step + 1) & 1, s, step + 1);
-                    if (step == 0 && more) fill(s + STAGES - 1);
-                } else if (s + 1 < slices) {
+                    if (step == 0) fill(s + STAGES - 1);
+                } else {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    wait_slices(more ? STAGES - 2 : slices - 2 - s);
+                    wait_loads<(STAGES - 2) * LPS>();
                     __builtin_amdgcn_s_barrier();
                     read(0, s + 1, 0);
                 }
                 multiply(step & 1);
+                interleave();
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        for (; s < slices; ++s) {
+#pragma unroll
+            for (int step = 0; step < STEPS; ++step) {
+                if (step + 1 < STEPS) read((step + 1) & 1, s, step + 1);
+                else if (s + 1 < slices) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    wait_slices(slices - 2 - s);
+                    __builtin_amdgcn_s_barrier();
+                    read(0, s + 1, 0);
+                }
+                multiply(step & 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+
+    // a step's LDS reads one or two behind each of its first matrix instructions
+    static __device__ __forceinline__ void interleave()
+    {
+        constexpr int M = TMI * TNI * (E::SIZE == 2 ? 1 : 4), R = E::SIZE == 2 ? (ACOL ? 2 : 1) * TMI + (BCOL ? 2 : 1) * TNI : (ACOL ? 4 : 1) * TMI + (BCOL ? 4 : 1) * TNI;
+        constexpr int EACH = (R + M - 2) / (M > 1 ? M - 1 : 1) > 0 ? (R + M - 2) / (M > 1 ? M - 1 : 1) : 1;
+#pragma unroll
+        for (int i = 0; i < (R + EACH - 1) / EACH; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
     }
 };
 
