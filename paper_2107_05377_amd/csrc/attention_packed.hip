@@ -19,6 +19,7 @@
 #include "packed_tile.h"
 #include "packed.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace mt {
@@ -146,34 +147,45 @@ __device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsign
 // ---- sequences
 struct Seq {
     int q0, lq, k0, lk, tile;
+    int chunk, chunks, first;       // of keys: this one's, how many the sequence has, the number of the tile's first item
 };
 __device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v, 0), total); }
 
-// The sequence and tile that workgroup w of a list of tiles (`tile` rows each, `per` rows per token, of the queries or of the keys) works on; false
-// behind the last.  Starts outside the arrays are brought inside, a sequence that would end before it starts is empty.
-__device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, int tile, bool keys, Seq& s)
+// Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with CHUNKED
+// its sequence's chunks of `keys_each` keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are brought
+// inside, a sequence that would end before it starts is empty.
+template <bool KEYS, bool BY_TILE = false>
+__device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, int tile, int keys_each, Seq& s)
 {
     const int lane = threadIdx.x & 63;
-    const int32_t* start = keys ? p.k_start : p.q_start;
-    const int total = keys ? p.total_k : p.total_q;
-    int base = 0;
+    const int32_t* start = KEYS ? p.k_start : p.q_start;
+    const int total = KEYS ? p.total_k : p.total_q;
+    int base = 0, base_items = 0;
     for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
         const int b = min(b0 + lane, p.n_seqs - 1);
         const int a = clamp_start(start[b], total), e = clamp_start(start[b + 1], total);
-        const int n = b0 + lane < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
-        int sum = n;
+        const int tiles = b0 + lane < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
+        int chunks = 1;
+        if (keys_each > 0) chunks = max(1, (max(clamp_start(p.k_start[b + 1], p.total_k) - clamp_start(p.k_start[b], p.total_k), 0) + keys_each - 1) / keys_each);
+        const int n = BY_TILE ? tiles : tiles * chunks;
+        int sum = n, items = tiles * chunks;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int up = __shfl_up(sum, o);
-            if (lane >= o) sum += up;
+            const int up = __shfl_up(sum, o), up_items = BY_TILE ? __shfl_up(items, o) : 0;
+            if (lane >= o) {
+                sum += up;
+                items += up_items;
+            }
         }
         const int all = __shfl(sum, 63);
         if (w < base + all) {
             const uint64_t past = __ballot(base + sum > w);
             const int l = __ffsll((unsigned long long)past) - 1;
-            const int bb = b0 + l;
-            const int first = base + __shfl(sum, l) - __shfl(n, l);
-            s.tile = w - first;
+            const int bb = b0 + l, mine = w - (base + __shfl(sum, l) - __shfl(n, l));
+            s.chunks = __shfl(chunks, l);
+            s.tile = BY_TILE ? mine : mine / s.chunks;
+            s.chunk = BY_TILE ? 0 : mine - s.tile * s.chunks;
+            s.first = BY_TILE ? base_items + __shfl(items, l) - __shfl(tiles, l) * s.chunks + s.tile * s.chunks : w - s.chunk;
             s.q0 = clamp_start(p.q_start[bb], p.total_q);
             s.lq = max(clamp_start(p.q_start[bb + 1], p.total_q) - s.q0, 0);
             s.k0 = clamp_start(p.k_start[bb], p.total_k);
@@ -181,6 +193,7 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
             return true;
         }
         base += all;
+        if (BY_TILE) base_items += __shfl(items, 63);
     }
     return false;
 }
@@ -254,31 +267,52 @@ __device__ __forceinline__ void store_cols(const f32x16 (&acc)[DP / 32], float b
         }
 }
 
-constexpr int kTileKeys = 64;
+// RW x KW wavefronts: RW blocks of 32 rows, each with KW wavefronts that take UB blocks of 32 keys of a tile in turn and put their sums together at the
+// end.  p.work: with keys_each > 0 a tile's keys are dealt out to workgroups as well, whose sums a second launch puts together.
+template <typename E, int DP, int RW, int KW, int UB>
+struct Forward {
+    using T = Tile<E, DP>;
+    static constexpr int BM = RW * 32, TK = KW * UB * 32, NW = RW * KW, BYTES = TK * T::ROWB, LDS = 4 * BYTES;
+    static constexpr int ROW = DP + 4;                      // floats of a partial row: sums, then reference and sum of the weights
+    static_assert(LDS <= 160 * 1024 && (KW - 1) * RW * (DP / 2 + 2) * 64 * 4 <= LDS, "");
+};
 
-template <typename E, int DP, int NW>
-__global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
+template <typename E, int DP, int RW, int KW, int UB>
+__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_forward_kernel(PackedAttn p, int keys_each)
 {
+    using F = Forward<E, DP, RW, KW, UB>;
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
-    constexpr int BM = NW * 32, TK = kTileKeys, BYTES = TK * T::ROWB;
+    constexpr int BM = F::BM, TK = F::TK, NW = F::NW, BYTES = F::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of keys and values
     const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
+    if (!find_tile<false>(p, blockIdx.x, group, BM, keys_each, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
     const int r0 = (tiles - 1 - s.tile) * BM;                                 // the rows that see most first
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;                    // query i sees keys up to i + shift
     const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
-    const int my_row = min(r0 + wave * 32 + l32, rows - 1);
+    const int my_row = min(r0 + rw * 32 + l32, rows - 1);
     const int tok = my_row / group, head = kvh * group + my_row - tok * group;
-    const int limit = limit_of(my_row), wave_min = limit_of(r0 + wave * 32), wave_max = limit_of(r0 + wave * 32 + 31);
-    const int n_keys = limit_of(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
+    const int limit = limit_of(my_row), wave_min = limit_of(r0 + rw * 32), wave_max = limit_of(r0 + rw * 32 + 31);
+    int n_keys = limit_of(r0 + BM - 1) + 1, t0 = 0;
+    if (keys_each > 0) {
+        t0 = s.chunk * (keys_each / TK);
+        n_keys = min(n_keys, (s.chunk + 1) * keys_each);
+    }
+    const int n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    const auto fetch = [&](int kt) {
+        const uint32_t to = lds0 + ((kt - t0) & 1) * 2 * BYTES;
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, kt * TK, s.lk - 1, p.d, to);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, kt * TK, s.lk - 1, p.d, to + BYTES);
+    };
+    if (t0 < n_tiles) fetch(t0);
     typename E::frag qf[DP / E::KS];
     load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
 
@@ -290,35 +324,27 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
     const float c = p.scale * kLog2e;
     float ref = -INFINITY, sum = 0.f;       // weights are exp2(c (score - ref))
 
-    if (n_tiles > 0) {
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds0);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds0 + BYTES);
-    }
     loaded(qf);
-    for (int kt = 0; kt < n_tiles; ++kt) {
+    for (int kt = t0; kt < n_tiles; ++kt) {
         loads_landed();
-        const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
+        const unsigned char* tk = lds + ((kt - t0) & 1) * 2 * BYTES + kw * UB * 32 * T::ROWB;
         const unsigned char* tv = tk + BYTES;
-        if (kt + 1 < n_tiles) {
-            const uint32_t next = lds0 + ((kt + 1) & 1) * 2 * BYTES;
-            stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
-            stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
-        }
-        const int key0 = kt * TK;
+        if (kt + 1 < n_tiles) fetch(kt + 1);
+        const int key0 = kt * TK + kw * UB * 32;
         if (key0 > wave_max) continue;
-        f32x16 sc[TK / 32];
+        f32x16 sc[UB];
 #pragma unroll
-        for (int u = 0; u < TK / 32; ++u) {
+        for (int u = 0; u < UB; ++u) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < DP / E::KS; ++ks) sc[u] = E::mma(T::row_frag(tk, u * 32 + l32, ks, half), qf[ks], sc[u]);
         }
-        const bool cut = key0 + TK - 1 > wave_min;
-        uint32_t seen[TK / 32];
+        const bool cut = key0 + UB * 32 - 1 > wave_min;
+        uint32_t seen[UB];
         if (cut) {
 #pragma unroll
-            for (int u = 0; u < TK / 32; ++u) {
+            for (int u = 0; u < UB; ++u) {
                 seen[u] = 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -330,7 +356,7 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
         }
         float top = sc[0][0];
 #pragma unroll
-        for (int u = 0; u < TK / 32; ++u)
+        for (int u = 0; u < UB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
         top = lane_pair_max<32>(top);
@@ -348,27 +374,121 @@ __global__ __launch_bounds__(NW * 64) void packed_forward_kernel(PackedAttn p)
         }
         const float rc = ref == -INFINITY ? 0.f : ref * c;
 #pragma unroll
-        for (int u = 0; u < TK / 32; ++u)
+        for (int u = 0; u < UB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 sc[u][i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i], c, -rc));
                 sum += sc[u][i];
             }
 #pragma unroll
-        for (int u = 0; u < TK / 32; ++u) add_product<E, DP, false>(acc, tv, u * 32, sc[u], cut, seen[u], lane);
+        for (int u = 0; u < UB; ++u) add_product<E, DP, false>(acc, tv, u * 32, sc[u], cut, seen[u], lane);
     }
     sum = lane_pair_sum<32>(sum);
-    if (r0 + wave * 32 + l32 < rows) {
-        const float by = limit < 0 ? 0.f : 1.f / sum;
-        if (limit < 0) {
+    if constexpr (KW > 1) {
+        // the wavefronts of a block of rows, in order
+        float* const other = reinterpret_cast<float*>(lds) + rw * (KW - 1) * (DP / 2 + 2) * 64 + lane;
+        __syncthreads();
+        if (kw > 0) {
+            float* at = other + (kw - 1) * (DP / 2 + 2) * 64;
 #pragma unroll
             for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+                for (int i = 0; i < 16; ++i) at[(db * 16 + i) * 64] = acc[db][i];
+            at[DP / 2 * 64] = ref;
+            at[(DP / 2 + 1) * 64] = sum;
         }
-        store_cols<E, DP>(acc, by, static_cast<elem*>(p.out) + (int64_t)(s.q0 + tok) * p.o_row + head * p.o_head, p.d, half);
-        if (p.lse && half == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
+        __syncthreads();
+        if (kw > 0) return;
+#pragma unroll 1
+        for (int o = 0; o < KW - 1; ++o) {
+            const float* at = other + o * (DP / 2 + 2) * 64;
+            const float ref_o = at[DP / 2 * 64], to = fmaxf(ref, ref_o), from = to == -INFINITY ? 0.f : to;
+            const float by = __builtin_amdgcn_exp2f((ref - from) * c), by_o = __builtin_amdgcn_exp2f((ref_o - from) * c);
+            ref = to;
+            sum = fmaf(at[(DP / 2 + 1) * 64], by_o, sum * by);
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] = fmaf(at[(db * 16 + i) * 64], by_o, acc[db][i] * by);
+        }
     }
+    if (r0 + rw * 32 + l32 >= rows) return;
+    if (s.chunks > 1) {
+        float* at = static_cast<float*>(p.work) + (((int64_t)(s.first + s.chunk) * p.kv_heads + kvh) * BM + rw * 32 + l32) * F::ROW;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = acc[db][g * 4 + j];
+                *reinterpret_cast<f32x4*>(at + db * 32 + g * 8 + half * 4) = v;
+            }
+        if (half == 0) {
+            at[DP] = ref;
+            at[DP + 1] = sum;
+        }
+        return;
+    }
+    if (limit < 0) {
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+    }
+    store_cols<E, DP>(acc, limit < 0 ? 0.f : 1.f / sum, static_cast<elem*>(p.out) + (int64_t)(s.q0 + tok) * p.o_row + head * p.o_head, p.d, half);
+    if (p.lse && half == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
+}
+
+// the chunks of a tile's keys put together, one workgroup per 4 rows of a tile and key head: 64 lanes a row
+template <typename E, int DP, int BM>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys_each)
+{
+    typedef typename E::elem elem;
+    constexpr int ROW = DP + 4, COLS = DP / 64;
+    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    Seq s;
+    if (!find_tile<false, true>(p, blockIdx.x, group, BM, keys_each, s) || s.chunks == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r = blockIdx.z * 4 + wave, row = (tiles - 1 - s.tile) * BM + r;
+    if (row >= rows) return;
+    const int tok = row / group, head = kvh * group + row - tok * group;
+    const int limit = min(tok + (p.causal ? s.lk - s.lq : 0x40000000), s.lk - 1);
+    const float c = p.scale * kLog2e;
+    const float* at = static_cast<const float*>(p.work) + (((int64_t)s.first * p.kv_heads + kvh) * BM + r) * ROW;
+    const int64_t step = (int64_t)p.kv_heads * BM * ROW;
+    float ref = -INFINITY;
+    for (int k = lane; k < s.chunks; k += 64) ref = fmaxf(ref, at[k * step + DP]);
+    ref = wave_max(ref);
+    const float from = ref == -INFINITY ? 0.f : ref;
+    float sum = 0.f, v[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) v[i] = 0.f;
+    for (int k0 = 0; k0 < s.chunks; k0 += 8) {
+        float x[8][COLS], ro[8], so[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float* from_k = at + min(k0 + k, s.chunks - 1) * step;
+            ro[k] = from_k[DP];
+            so[k] = from_k[DP + 1];
+#pragma unroll
+            for (int i = 0; i < COLS; ++i) x[k][i] = from_k[lane * COLS + i];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float by = k0 + k < s.chunks ? __builtin_amdgcn_exp2f((ro[k] - from) * c) : 0.f;
+            if (k0 + k >= s.chunks) continue;
+            sum = fmaf(so[k], by, sum);
+#pragma unroll
+            for (int i = 0; i < COLS; ++i) v[i] = fmaf(x[k][i], by, v[i]);
+        }
+    }
+    const float by = limit < 0 ? 0.f : 1.f / sum;
+    elem* out = static_cast<elem*>(p.out) + (int64_t)(s.q0 + tok) * p.o_row + head * p.o_head;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i)
+        if (lane * COLS + i < p.d) out[lane * COLS + i] = (elem)(limit < 0 ? 0.f : v[i] * by);
+    if (p.lse && lane == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
 }
 
 // What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and delta = dctx . ctx.  8 lanes a row.
@@ -398,7 +518,7 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* 
 
 // dq: rows fixed, keys pass by
 template <typename E, int DP, int NW>
-__global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const float* stat)
+__global__ __launch_bounds__(NW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
 {
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
@@ -407,7 +527,7 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
     const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile(p, blockIdx.x, group, BM, false, s)) return;
+    if (!find_tile<false>(p, blockIdx.x, group, BM, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
     const int r0 = (tiles - 1 - s.tile) * BM;
@@ -479,28 +599,39 @@ __global__ __launch_bounds__(NW * 64) void packed_dq_kernel(PackedAttn p, const 
         store_cols<E, DP>(acc, p.scale, static_cast<elem*>(p.dq) + (int64_t)(s.q0 + tok) * p.dq_row + head * p.dq_head, p.d, half);
 }
 
-// dk, dv: keys fixed, the rows of all heads of the group pass by
-template <typename E, int DP, int NW, int TQ>
-__global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
+// dk, dv: keys fixed, the rows of all heads of the group pass by.  KW blocks of 32 keys, each with RW wavefronts that take one block of 32 rows of a tile
+// each and put their sums together at the end.
+template <typename E, int DP, int KW, int RW>
+struct KeyGrad {
+    using T = Tile<E, DP>;
+    static constexpr int NW = KW * RW, BN = KW * 32, TQ = RW * 32, BYTES = TQ * T::ROWB;
+    static constexpr int LDS = std::max(4 * BYTES + 2 * TQ * 12, KW * (RW - 1) * DP * 64 * 4);
+    static_assert(LDS <= 160 * 1024, "");
+};
+
+template <typename E, int DP, int KW, int RW>
+__global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
 {
+    using G = KeyGrad<E, DP, KW, RW>;
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
-    constexpr int BN = NW * 32, BYTES = TQ * T::ROWB;
+    constexpr int BN = G::BN, TQ = G::TQ, NW = G::NW, BYTES = G::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of rows of q and dctx; their statistics
+    const uint32_t lds0 = lds_address(lds);
     struct RowInfo {
         float lse[TQ], delta[TQ];
         int limit[TQ];
     };
     RowInfo* const info = reinterpret_cast<RowInfo*>(lds + 4 * BYTES);
-    const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile(p, blockIdx.x, 1, BN, true, s)) return;
+    if (!find_tile<true>(p, blockIdx.x, 1, BN, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int kw = wave / RW, rw = wave % RW;
     const int rows = s.lq * group, n0 = s.tile * BN;
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;
-    const int my_key = n0 + wave * 32 + l32, key = min(my_key, s.lk - 1);
-    const int wave_last = min(n0 + wave * 32 + 31, s.lk - 1), wave_first = n0 + wave * 32;
+    const int my_key = n0 + kw * 32 + l32, key = min(my_key, s.lk - 1);
+    const int wave_last = min(n0 + kw * 32 + 31, s.lk - 1), wave_first = n0 + kw * 32;
     // the first query that sees the tile's first key
     const int t_first = p.causal ? min(max(n0 - shift, 0), s.lq) : 0;
     const int rt0 = t_first * group / TQ, n_tiles = (rows + TQ - 1) / TQ;
@@ -509,7 +640,7 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
     load_row<E, DP>(kf, static_cast<const elem*>(p.k) + (int64_t)(s.k0 + key) * p.k_row + kvh * p.k_head, p.d, half);
     load_row<E, DP>(vf, static_cast<const elem*>(p.v) + (int64_t)(s.k0 + key) * p.v_row + kvh * p.v_head, p.d, half);
     const elem* Q = static_cast<const elem*>(p.q) + (int64_t)s.q0 * p.q_row + (int64_t)kvh * group * p.q_head;
-    const elem* G = static_cast<const elem*>(p.dctx) + (int64_t)s.q0 * p.g_row + (int64_t)kvh * group * p.g_head;
+    const elem* O = static_cast<const elem*>(p.dctx) + (int64_t)s.q0 * p.g_row + (int64_t)kvh * group * p.g_head;
     const float c = p.scale * kLog2e;
 
     f32x16 ak[DP / 32], av[DP / 32];
@@ -523,7 +654,7 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
     int r_limit = -1;
     const auto fetch = [&](int rt, uint32_t to) {
         stage<E, DP, TQ, NW, true>(Q, p.q_row, p.q_head, group, rt * TQ, rows - 1, p.d, to);
-        stage<E, DP, TQ, NW, true>(G, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
+        stage<E, DP, TQ, NW, true>(O, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
         if (threadIdx.x < TQ) {
             const int r = rt * TQ + threadIdx.x, rr = min(r, rows - 1);
             r_lse = my_stat[rr];
@@ -552,19 +683,17 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
         const RowInfo& in = info[at];
         const bool more = rt + 1 < n_tiles;
         if (more) fetch(rt + 1, lds0 + (at ^ 1) * 2 * BYTES);
-#pragma unroll
-        for (int u = 0; u < TQ / 32; ++u) {
-            const int b0 = rt * TQ + u * 32;
-            // the block's last row sees most
-            const int last_limit = min(min(b0 + 31, rows - 1) / group + shift, s.lk - 1), first_limit = min(b0 / group + shift, s.lk - 1);
-            if (b0 >= rows || wave_first > last_limit) continue;
+        const int b0 = rt * TQ + rw * 32;
+        // the block's last row sees most
+        const int last_limit = min(min(b0 + 31, rows - 1) / group + shift, s.lk - 1), first_limit = min(b0 / group + shift, s.lk - 1);
+        if (b0 < rows && wave_first <= last_limit) {
             f32x16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < DP / E::KS; ++ks) {
-                sc = E::mma(T::row_frag(tq, u * 32 + l32, ks, half), kf[ks], sc);
-                dp = E::mma(T::row_frag(tg, u * 32 + l32, ks, half), vf[ks], dp);
+                sc = E::mma(T::row_frag(tq, rw * 32 + l32, ks, half), kf[ks], sc);
+                dp = E::mma(T::row_frag(tg, rw * 32 + l32, ks, half), vf[ks], dp);
             }
             const bool cut = wave_last > first_limit || b0 + 32 > rows;
             uint32_t seen = 0xFFFFu;
@@ -573,11 +702,11 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[u * 32 + 8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
+                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[rw * 32 + 8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[u * 32 + 8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[u * 32 + 8 * g + 4 * half]);
+                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[rw * 32 + 8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[rw * 32 + 8 * g + 4 * half]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * g + j;
@@ -592,10 +721,37 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
                     dp[i] = (seen >> i) & 1 ? dp[i] : 0.f;
                 }
             }
-            add_product<E, DP, false>(av, tg, u * 32, sc, cut, seen, lane);
-            add_product<E, DP, true>(ak, tq, u * 32, dp, cut, seen, lane);
+            add_product<E, DP, false>(av, tg, rw * 32, sc, cut, seen, lane);
+            add_product<E, DP, true>(ak, tq, rw * 32, dp, cut, seen, lane);
         }
         if (more) keep(info[at ^ 1]);
+    }
+    if constexpr (RW > 1) {
+        float* const other = reinterpret_cast<float*>(lds) + kw * (RW - 1) * DP * 64 + lane;
+        __syncthreads();
+        if (rw > 0) {
+            float* to = other + (rw - 1) * DP * 64;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    to[(db * 16 + i) * 64] = ak[db][i];
+                    to[(DP / 2 + db * 16 + i) * 64] = av[db][i];
+                }
+        }
+        __syncthreads();
+        if (rw > 0) return;
+#pragma unroll 1
+        for (int o = 0; o < RW - 1; ++o) {
+            const float* from = other + o * DP * 64;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    ak[db][i] += from[(db * 16 + i) * 64];
+                    av[db][i] += from[(DP / 2 + db * 16 + i) * 64];
+                }
+        }
     }
     if (my_key < s.lk) {
         store_cols<E, DP>(ak, p.scale, static_cast<elem*>(p.dk) + (int64_t)(s.k0 + key) * p.dk_row + kvh * p.dk_head, p.d, half);
@@ -603,17 +759,56 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void p
     }
 }
 
-template <typename E, int DP, int NW>
-hipError_t forward_with(const PackedAttn& p, hipStream_t stream)
+// ---- launches
+// How the rows of the forward pass are dealt out.
+struct Deal {
+    int rows_each;          // rows of a workgroup: 32, 64 or 128
+    int keys_each;          // > 0: keys of a workgroup
+    int64_t items, tiles;   // workgroups per key head; tiles
+};
+Deal deal_of(int n_seqs, int total_q, int total_k, int heads, int kv_heads)
 {
+    const int64_t group = heads / kv_heads, rows = total_q * group;
+    Deal d{128, 0, 0, 0};
+    const auto tiles = [&](int bm) { return rows / bm + n_seqs; };
+    if (rows <= 32ll * n_seqs) d.rows_each = 32;
+    else if (rows <= 96ll * n_seqs || tiles(128) * kv_heads < 2048) d.rows_each = 64;
+    d.tiles = tiles(d.rows_each);
+    d.items = d.tiles;
+    if (d.rows_each == 32 && d.tiles * kv_heads < 1024) {
+        // few workgroups: keys dealt out so that there are about 1024, 256 keys each at least (what a workgroup needs to get going costs as much)
+        const int64_t each = std::max<int64_t>(256, ((int64_t)total_k * kv_heads / 1024 + 255) / 256 * 256);
+        if (total_k > each) {
+            d.keys_each = (int)each;
+            // sum over sequences of (rows / 32 + 1) (keys / each + 1)
+            d.items = (rows / 32) * (total_k / each) + rows / 32 + total_k / each + n_seqs;
+        }
+    }
+    return d;
+}
+
+template <typename E, int DP, int RW, int KW, int UB>
+hipError_t forward_with(const PackedAttn& p, const Deal& d, hipStream_t stream)
+{
+    using F = Forward<E, DP, RW, KW, UB>;
     static std::atomic<uint64_t> done{0};
-    const int bytes = 4 * kTileKeys * Tile<E, DP>::ROWB;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, NW>), bytes, done);
+    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, RW, KW, UB>), F::LDS, done);
     if (e != hipSuccess) return e;
-    const int64_t tiles = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
-    if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
-    packed_forward_kernel<E, DP, NW><<<dim3((unsigned)tiles, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p);
+    if (d.items > 0x7FFFFFFF) return hipErrorInvalidValue;
+    packed_forward_kernel<E, DP, RW, KW, UB><<<dim3((unsigned)d.items, (unsigned)p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
+    if ((e = hipGetLastError()) != hipSuccess || d.keys_each == 0) return e;
+    const int rows = std::min<int64_t>(F::BM, (int64_t)p.total_q * (p.heads / p.kv_heads));
+    packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)d.tiles, (unsigned)p.kv_heads, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each);
     return hipGetLastError();
+}
+template <typename E, int DP>
+hipError_t forward_of(const PackedAttn& p, hipStream_t stream)
+{
+    const Deal d = deal_of(p.n_seqs, p.total_q, p.total_k, p.heads, p.kv_heads);
+    constexpr bool WIDE = Tile<E, DP>::ROWB == 512;         // float32, 128 columns: half the keys a tile
+    if (d.rows_each == 32) return forward_with<E, DP, 1, WIDE ? 2 : 4, 1>(p, d, stream);
+    if (d.rows_each == 64) return forward_with<E, DP, 2, 2, E::SIZE == 2 && DP == 64 ? 2 : 1>(p, d, stream);
+    return forward_with<E, DP, 4, 1, 2>(p, d, stream);
 }
 
 template <typename E, int DP>
@@ -621,20 +816,20 @@ hipError_t gradient_with(const PackedAttn& p, hipStream_t stream)
 {
     constexpr int NW = 4;
     static std::atomic<uint64_t> done_q{0}, done_k{0};
-    constexpr int TQ = E::SIZE == 2 && DP == 64 ? 64 : 32;
-    const int bytes = 4 * 32 * Tile<E, DP>::ROWB, bytes_k = 4 * TQ * Tile<E, DP>::ROWB + 2 * TQ * 12;
+    using G = KeyGrad<E, DP, 2, 2>;
+    const int bytes = 4 * 32 * Tile<E, DP>::ROWB;
     hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, NW>), bytes, done_q);
     if (e != hipSuccess) return e;
-    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, NW, TQ>), bytes_k, done_k);
+    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, 2, 2>), G::LDS, done_k);
     if (e != hipSuccess) return e;
     float* stat = static_cast<float*>(p.work);
     const int64_t n = (int64_t)p.total_q * p.heads;
     const int64_t tiles_q = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
-    const int64_t tiles_k = ((int64_t)p.total_k + NW * 32 - 1) / (NW * 32) + p.n_seqs;
+    const int64_t tiles_k = ((int64_t)p.total_k + G::BN - 1) / G::BN + p.n_seqs;
     if (tiles_q > 0x7FFFFFFF || tiles_k > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
     packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dkv_kernel<E, DP, NW, TQ><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), NW * 64, bytes_k, stream>>>(p, stat);
+    packed_dkv_kernel<E, DP, 2, 2><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     packed_dq_kernel<E, DP, NW><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p, stat);
     return hipGetLastError();
@@ -642,13 +837,17 @@ hipError_t gradient_with(const PackedAttn& p, hipStream_t stream)
 
 }  // namespace
 
-size_t packed_attention_work(int, int, int, int, int, int, int) { return 0; }
+size_t packed_attention_work(int n_seqs, int total_q, int total_k, int heads, int kv_heads, int d)
+{
+    const Deal deal = deal_of(n_seqs, total_q, total_k, heads, kv_heads);
+    return deal.keys_each ? (size_t)deal.items * kv_heads * deal.rows_each * ((d <= 64 ? 64 : 128) + 4) * 4 : 0;
+}
 size_t packed_attention_grad_work(int total_q, int heads) { return (size_t)total_q * heads * 8; }
 
 hipError_t launch_packed_attention(const PackedAttn& p, int f32, hipStream_t stream)
 {
-    if (f32) return p.d <= 64 ? forward_with<F32, 64, 4>(p, stream) : forward_with<F32, 128, 4>(p, stream);
-    return p.d <= 64 ? forward_with<B16, 64, 4>(p, stream) : forward_with<B16, 128, 4>(p, stream);
+    if (f32) return p.d <= 64 ? forward_of<F32, 64>(p, stream) : forward_of<F32, 128>(p, stream);
+    return p.d <= 64 ? forward_of<B16, 64>(p, stream) : forward_of<B16, 128>(p, stream);
 }
 
 hipError_t launch_packed_attention_grad(const PackedAttn& p, int f32, hipStream_t stream)

@@ -67,7 +67,7 @@ PackedAttn attention_args(const mt_packed_attention* op)
 size_t attention_work(const mt_packed_attention* op, bool grad)
 {
     if (grad) return packed_attention_grad_work(op->total_q, op->heads);
-    return packed_attention_work(op->precision != MT_BF16, op->n_seqs, op->total_q, op->total_k, op->heads, op->kv_heads, op->width);
+    return packed_attention_work(op->n_seqs, op->total_q, op->total_k, op->heads, op->kv_heads, op->width);
 }
 
 }  // namespace

@@ -22,7 +22,7 @@ struct PackedAttn {
     void* work;
     size_t work_bytes;
 };
-size_t packed_attention_work(int f32, int n_seqs, int total_q, int total_k, int heads, int kv_heads, int d);
+size_t packed_attention_work(int n_seqs, int total_q, int total_k, int heads, int kv_heads, int d);
 size_t packed_attention_grad_work(int total_q, int heads);
 hipError_t launch_packed_attention(const PackedAttn& p, int f32, hipStream_t stream);
 hipError_t launch_packed_attention_grad(const PackedAttn& p, int f32, hipStream_t stream);
