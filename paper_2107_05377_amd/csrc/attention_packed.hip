@@ -151,20 +151,23 @@ struct Seq {
 };
 __device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v, 0), total); }
 
-// Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with CHUNKED
-// its sequence's chunks of `keys_each` keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are brought
-// inside, a sequence that would end before it starts is empty.
-template <bool KEYS, bool BY_TILE = false>
+// Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with
+// keys_each > 0 its sequence's chunks of that many keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are
+// brought inside, a sequence that would end before it starts is empty.  A workgroup looks through 64 sequences for each of its wavefronts at a time:
+// one load and a prefix sum, about a microsecond in which nothing else happens.
+template <int NW, bool KEYS, bool BY_TILE = false>
 __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, int tile, int keys_each, Seq& s)
 {
-    const int lane = threadIdx.x & 63;
+    __shared__ int wave_sum[NW][2], found[5];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t* start = KEYS ? p.k_start : p.q_start;
     const int total = KEYS ? p.total_k : p.total_q;
     int base = 0, base_items = 0;
-    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
-        const int b = min(b0 + lane, p.n_seqs - 1);
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 64 * NW) {
+        const bool one = p.n_seqs - b0 <= 64;               // every wavefront looks at the same sequences: nothing to exchange
+        const int at = b0 + (one ? lane : (int)threadIdx.x), b = min(at, p.n_seqs - 1);
         const int a = clamp_start(start[b], total), e = clamp_start(start[b + 1], total);
-        const int tiles = b0 + lane < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
+        const int tiles = at < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
         int chunks = 1;
         if (keys_each > 0) chunks = max(1, (max(clamp_start(p.k_start[b + 1], p.total_k) - clamp_start(p.k_start[b], p.total_k), 0) + keys_each - 1) / keys_each);
         const int n = BY_TILE ? tiles : tiles * chunks;
@@ -177,23 +180,60 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
                 items += up_items;
             }
         }
-        const int all = __shfl(sum, 63);
+        int all = __shfl(sum, 63), all_items = __shfl(items, 63);
+        if (!one) {
+            if (lane == 63) {
+                wave_sum[wave][0] = sum;
+                wave_sum[wave][1] = items;
+            }
+            __syncthreads();
+            int before = 0, before_items = 0;
+            all = all_items = 0;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                before += k < wave ? wave_sum[k][0] : 0;
+                before_items += k < wave ? wave_sum[k][1] : 0;
+                all += wave_sum[k][0];
+                all_items += wave_sum[k][1];
+            }
+            sum += before;
+            items += before_items;
+        }
         if (w < base + all) {
-            const uint64_t past = __ballot(base + sum > w);
-            const int l = __ffsll((unsigned long long)past) - 1;
-            const int bb = b0 + l, mine = w - (base + __shfl(sum, l) - __shfl(n, l));
-            s.chunks = __shfl(chunks, l);
+            int seq, mine, first_items, tiles_n;
+            if (one) {
+                const uint64_t past = __ballot(base + sum > w);
+                const int l = __ffsll((unsigned long long)past) - 1;
+                seq = b0 + l;
+                mine = w - (base + __shfl(sum, l) - __shfl(n, l));
+                s.chunks = __shfl(chunks, l);
+                tiles_n = __shfl(tiles, l);
+                first_items = base_items + __shfl(items, l) - tiles_n * s.chunks;
+            } else {
+                if (w >= base + sum - n && w < base + sum) {
+                    found[0] = at;
+                    found[1] = w - (base + sum - n);
+                    found[2] = chunks;
+                    found[3] = base_items + items - tiles * chunks;
+                }
+                __syncthreads();
+                seq = found[0];
+                mine = found[1];
+                s.chunks = found[2];
+                first_items = found[3];
+            }
             s.tile = BY_TILE ? mine : mine / s.chunks;
             s.chunk = BY_TILE ? 0 : mine - s.tile * s.chunks;
-            s.first = BY_TILE ? base_items + __shfl(items, l) - __shfl(tiles, l) * s.chunks + s.tile * s.chunks : w - s.chunk;
-            s.q0 = clamp_start(p.q_start[bb], p.total_q);
-            s.lq = max(clamp_start(p.q_start[bb + 1], p.total_q) - s.q0, 0);
-            s.k0 = clamp_start(p.k_start[bb], p.total_k);
-            s.lk = max(clamp_start(p.k_start[bb + 1], p.total_k) - s.k0, 0);
+            s.first = BY_TILE ? first_items + s.tile * s.chunks : w - s.chunk;
+            s.q0 = clamp_start(p.q_start[seq], p.total_q);
+            s.lq = max(clamp_start(p.q_start[seq + 1], p.total_q) - s.q0, 0);
+            s.k0 = clamp_start(p.k_start[seq], p.total_k);
+            s.lk = max(clamp_start(p.k_start[seq + 1], p.total_k) - s.k0, 0);
             return true;
         }
         base += all;
-        if (BY_TILE) base_items += __shfl(items, 63);
+        base_items += all_items;
+        __syncthreads();
     }
     return false;
 }
@@ -223,9 +263,20 @@ __device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_
     }
 }
 
-__device__ __forceinline__ void loads_landed()
+// The tiles that pass by go through a ring in LDS: one is used while up to STAGES - 1 are under way.  All loads of a loop are those of its ring, LPS of each
+// wavefront per tile, so that a wait can leave the last tiles under way.
+template <int N>
+__device__ __forceinline__ void wait_loads()
 {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+template <int STAGES, int LPS>
+__device__ __forceinline__ void tile_landed(int behind)         // tiles behind this one that have been asked for
+{
+    static_assert(STAGES >= 2 && STAGES <= 4 && (STAGES - 2) * LPS < 64, "");
+    if (STAGES >= 4 && behind >= 2) wait_loads<(STAGES >= 4 ? 2 : 0) * LPS>();
+    else if (STAGES >= 3 && behind >= 1) wait_loads<(STAGES >= 3 ? 1 : 0) * LPS>();
+    else wait_loads<0>();
     __syncthreads();
 }
 
@@ -269,26 +320,26 @@ __device__ __forceinline__ void store_cols(const f32x16 (&acc)[DP / 32], float b
 
 // RW x KW wavefronts: RW blocks of 32 rows, each with KW wavefronts that take UB blocks of 32 keys of a tile in turn and put their sums together at the
 // end.  p.work: with keys_each > 0 a tile's keys are dealt out to workgroups as well, whose sums a second launch puts together.
-template <typename E, int DP, int RW, int KW, int UB>
+template <typename E, int DP, int RW, int KW, int UB, int STAGES>
 struct Forward {
     using T = Tile<E, DP>;
-    static constexpr int BM = RW * 32, TK = KW * UB * 32, NW = RW * KW, BYTES = TK * T::ROWB, LDS = 4 * BYTES;
+    static constexpr int BM = RW * 32, TK = KW * UB * 32, NW = RW * KW, BYTES = TK * T::ROWB, LDS = STAGES * 2 * BYTES, LPS = 2 * BYTES / 1024 / NW;
     static constexpr int ROW = DP + 4;                      // floats of a partial row: sums, then reference and sum of the weights
     static_assert(LDS <= 160 * 1024 && (KW - 1) * RW * (DP / 2 + 2) * 64 * 4 <= LDS, "");
 };
 
-template <typename E, int DP, int RW, int KW, int UB>
+template <typename E, int DP, int RW, int KW, int UB, int STAGES>
 __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_forward_kernel(PackedAttn p, int keys_each)
 {
-    using F = Forward<E, DP, RW, KW, UB>;
+    using F = Forward<E, DP, RW, KW, UB, STAGES>;
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
     constexpr int BM = F::BM, TK = F::TK, NW = F::NW, BYTES = F::BYTES;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of keys and values
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // the ring of keys and values
     const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile<false>(p, blockIdx.x, group, BM, keys_each, s)) return;
+    if (!find_tile<NW, false>(p, blockIdx.x, group, BM, keys_each, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
@@ -307,12 +358,14 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_f
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
-    const auto fetch = [&](int kt) {
-        const uint32_t to = lds0 + ((kt - t0) & 1) * 2 * BYTES;
+    const auto fetch = [&](int kt, int stage_at) {
+        const uint32_t to = lds0 + stage_at * 2 * BYTES;
         stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, kt * TK, s.lk - 1, p.d, to);
         stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, kt * TK, s.lk - 1, p.d, to + BYTES);
     };
-    if (t0 < n_tiles) fetch(t0);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (t0 + i < n_tiles) fetch(t0 + i, i);
     typename E::frag qf[DP / E::KS];
     load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
 
@@ -325,11 +378,12 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_f
     float ref = -INFINITY, sum = 0.f;       // weights are exp2(c (score - ref))
 
     loaded(qf);
-    for (int kt = t0; kt < n_tiles; ++kt) {
-        loads_landed();
-        const unsigned char* tk = lds + ((kt - t0) & 1) * 2 * BYTES + kw * UB * 32 * T::ROWB;
+    int at = 0;
+    for (int kt = t0; kt < n_tiles; ++kt, at = at + 1 == STAGES ? 0 : at + 1) {
+        tile_landed<STAGES, F::LPS>(n_tiles - 1 - kt);
+        if (kt + STAGES - 1 < n_tiles) fetch(kt + STAGES - 1, at == 0 ? STAGES - 1 : at - 1);
+        const unsigned char* tk = lds + at * 2 * BYTES + kw * UB * 32 * T::ROWB;
         const unsigned char* tv = tk + BYTES;
-        if (kt + 1 < n_tiles) fetch(kt + 1);
         const int key0 = kt * TK + kw * UB * 32;
         if (key0 > wave_max) continue;
         f32x16 sc[UB];
@@ -448,7 +502,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys
     constexpr int ROW = DP + 4, COLS = DP / 64;
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile<false, true>(p, blockIdx.x, group, BM, keys_each, s) || s.chunks == 1) return;
+    if (!find_tile<4, false, true>(p, blockIdx.x, group, BM, keys_each, s) || s.chunks == 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r = blockIdx.z * 4 + wave, row = (tiles - 1 - s.tile) * BM + r;
     if (row >= rows) return;
@@ -516,30 +570,47 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* 
     if (part == 1) stat[all + to] = sum;
 }
 
-// dq: rows fixed, keys pass by
-template <typename E, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
+// dq: rows fixed, keys pass by.  RW blocks of 32 rows, each with KW wavefronts that take a block of 32 keys of a tile each.
+template <typename E, int DP, int RW, int KW, int STAGES>
+struct RowGrad {
+    using T = Tile<E, DP>;
+    static constexpr int BM = RW * 32, TK = KW * 32, NW = RW * KW, BYTES = TK * T::ROWB, LDS = STAGES * 2 * BYTES, LPS = 2 * BYTES / 1024 / NW;
+    static_assert(LDS <= 160 * 1024 && (KW - 1) * RW * DP / 2 * 64 * 4 <= LDS, "");
+};
+
+template <typename E, int DP, int RW, int KW, int STAGES>
+__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
 {
+    using R = RowGrad<E, DP, RW, KW, STAGES>;
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
-    constexpr int BM = NW * 32, TK = 32, BYTES = TK * T::ROWB;
+    constexpr int BM = R::BM, TK = R::TK, NW = R::NW, BYTES = R::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile<false>(p, blockIdx.x, group, BM, 0, s)) return;
+    if (!find_tile<NW, false>(p, blockIdx.x, group, BM, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
     const int r0 = (tiles - 1 - s.tile) * BM;
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;
     const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
-    const int my_row = min(r0 + wave * 32 + l32, rows - 1);
+    const int my_row = min(r0 + rw * 32 + l32, rows - 1);
     const int tok = my_row / group, head = kvh * group + my_row - tok * group;
-    const int limit = limit_of(my_row), wave_min = limit_of(r0 + wave * 32), wave_max = limit_of(r0 + wave * 32 + 31);
+    const int limit = limit_of(my_row), wave_min = limit_of(r0 + rw * 32), wave_max = limit_of(r0 + rw * 32 + 31);
     const int n_keys = limit_of(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    const auto fetch = [&](int kt, int stage_at) {
+        const uint32_t to = lds0 + stage_at * 2 * BYTES;
+        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, kt * TK, s.lk - 1, p.d, to);
+        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, kt * TK, s.lk - 1, p.d, to + BYTES);
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < n_tiles) fetch(i, i);
     typename E::frag qf[DP / E::KS], gf[DP / E::KS];
     load_row<E, DP>(qf, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
     load_row<E, DP>(gf, static_cast<const elem*>(p.dctx) + (int64_t)(s.q0 + tok) * p.g_row + head * p.g_head, p.d, half);
@@ -552,33 +623,26 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_ker
     for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
-    if (n_tiles > 0) {
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, 0, s.lk - 1, p.d, lds0);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, 0, s.lk - 1, p.d, lds0 + BYTES);
-    }
     loaded(qf);
     loaded(gf);
     asm volatile("" ::"v"(lse), "v"(dl));
-    for (int kt = 0; kt < n_tiles; ++kt) {
-        loads_landed();
-        const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
+    int at = 0;
+    for (int kt = 0; kt < n_tiles; ++kt, at = at + 1 == STAGES ? 0 : at + 1) {
+        tile_landed<STAGES, R::LPS>(n_tiles - 1 - kt);
+        if (kt + STAGES - 1 < n_tiles) fetch(kt + STAGES - 1, at == 0 ? STAGES - 1 : at - 1);
+        const unsigned char* tk = lds + at * 2 * BYTES;
         const unsigned char* tv = tk + BYTES;
-        if (kt + 1 < n_tiles) {
-            const uint32_t next = lds0 + ((kt + 1) & 1) * 2 * BYTES;
-            stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next);
-            stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, (kt + 1) * TK, s.lk - 1, p.d, next + BYTES);
-        }
-        const int key0 = kt * TK;
+        const int key0 = kt * TK + kw * 32;
         if (key0 > wave_max) continue;
         f32x16 sc, dp;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < DP / E::KS; ++ks) {
-            sc = E::mma(T::row_frag(tk, l32, ks, half), qf[ks], sc);
-            dp = E::mma(T::row_frag(tv, l32, ks, half), gf[ks], dp);
+            sc = E::mma(T::row_frag(tk, kw * 32 + l32, ks, half), qf[ks], sc);
+            dp = E::mma(T::row_frag(tv, kw * 32 + l32, ks, half), gf[ks], dp);
         }
-        const bool cut = key0 + TK - 1 > wave_min;
+        const bool cut = key0 + 31 > wave_min;
         uint32_t seen = 0xFFFFu;
         if (cut) {
             seen = 0;
@@ -586,46 +650,58 @@ __global__ __launch_bounds__(NW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_ker
             for (int i = 0; i < 16; ++i) seen |= key0 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? 1u << i : 0u;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
-        }
+        for (int i = 0; i < 16; ++i) sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
         if (cut) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = (seen >> i) & 1 ? sc[i] : 0.f;
         }
-        add_product<E, DP, true>(acc, tk, 0, sc, cut, seen, lane);
+        add_product<E, DP, true>(acc, tk, kw * 32, sc, cut, seen, lane);
     }
-    if (r0 + wave * 32 + l32 < rows)
+    if constexpr (KW > 1) {
+        float* const other = reinterpret_cast<float*>(lds) + rw * (KW - 1) * DP / 2 * 64 + lane;
+        __syncthreads();
+        if (kw > 0) {
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) other[((kw - 1) * DP / 2 + db * 16 + i) * 64] = acc[db][i];
+        }
+        __syncthreads();
+        if (kw > 0) return;
+#pragma unroll 1
+        for (int o = 0; o < KW - 1; ++o)
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] += other[(o * DP / 2 + db * 16 + i) * 64];
+    }
+    if (r0 + rw * 32 + l32 < rows)
         store_cols<E, DP>(acc, p.scale, static_cast<elem*>(p.dq) + (int64_t)(s.q0 + tok) * p.dq_row + head * p.dq_head, p.d, half);
 }
 
 // dk, dv: keys fixed, the rows of all heads of the group pass by.  KW blocks of 32 keys, each with RW wavefronts that take one block of 32 rows of a tile
 // each and put their sums together at the end.
-template <typename E, int DP, int KW, int RW>
+template <typename E, int DP, int KW, int RW, int STAGES>
 struct KeyGrad {
     using T = Tile<E, DP>;
-    static constexpr int NW = KW * RW, BN = KW * 32, TQ = RW * 32, BYTES = TQ * T::ROWB;
-    static constexpr int LDS = std::max(4 * BYTES + 2 * TQ * 12, KW * (RW - 1) * DP * 64 * 4);
-    static_assert(LDS <= 160 * 1024, "");
+    // a stage: rows of q, rows of dctx, 256 bytes of every wavefront's: lse, delta and copies of them
+    static constexpr int NW = KW * RW, BN = KW * 32, TQ = RW * 32, BYTES = TQ * T::ROWB, STAGE = 2 * BYTES + NW * 256, LPS = 2 * BYTES / 1024 / NW + 1;
+    static constexpr int LDS = std::max(STAGES * STAGE, KW * (RW - 1) * DP * 64 * 4);
+    static_assert(LDS <= 160 * 1024 && TQ <= 64 && NW >= 2, "");
 };
 
-template <typename E, int DP, int KW, int RW>
+template <typename E, int DP, int KW, int RW, int STAGES>
 __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
 {
-    using G = KeyGrad<E, DP, KW, RW>;
+    using G = KeyGrad<E, DP, KW, RW, STAGES>;
     using T = Tile<E, DP>;
     typedef typename E::elem elem;
     constexpr int BN = G::BN, TQ = G::TQ, NW = G::NW, BYTES = G::BYTES;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // two stages of rows of q and dctx; their statistics
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
-    struct RowInfo {
-        float lse[TQ], delta[TQ];
-        int limit[TQ];
-    };
-    RowInfo* const info = reinterpret_cast<RowInfo*>(lds + 4 * BYTES);
     const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
     Seq s;
-    if (!find_tile<true>(p, blockIdx.x, 1, BN, 0, s)) return;
+    if (!find_tile<NW, true>(p, blockIdx.x, 1, BN, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int kw = wave / RW, rw = wave % RW;
     const int rows = s.lq * group, n0 = s.tile * BN;
@@ -649,40 +725,27 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
 #pragma unroll
         for (int i = 0; i < 16; ++i) ak[db][i] = av[db][i] = 0.f;
 
-    const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group;
-    float r_lse = 0.f, r_delta = 0.f;
-    int r_limit = -1;
-    const auto fetch = [&](int rt, uint32_t to) {
+    // wavefronts 0, 2 .. fetch lse, 1, 3 .. delta
+    const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group + (wave & 1) * (int64_t)p.total_q * p.heads;
+    const auto fetch = [&](int rt, int stage_at) {
+        const uint32_t to = lds0 + stage_at * G::STAGE;
         stage<E, DP, TQ, NW, true>(Q, p.q_row, p.q_head, group, rt * TQ, rows - 1, p.d, to);
         stage<E, DP, TQ, NW, true>(O, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
-        if (threadIdx.x < TQ) {
-            const int r = rt * TQ + threadIdx.x, rr = min(r, rows - 1);
-            r_lse = my_stat[rr];
-            r_delta = my_stat[rr + (int64_t)p.total_q * p.heads];
-            r_limit = r < rows ? min(rr / group + shift, s.lk - 1) : -1;
-        }
+        load_to_lds_4(my_stat + min(rt * TQ + lane, rows - 1), to + 2 * BYTES + wave * 256);
     };
-    const auto keep = [&](RowInfo& i) {
-        if (threadIdx.x < TQ) {
-            i.lse[threadIdx.x] = r_lse;
-            i.delta[threadIdx.x] = r_delta;
-            i.limit[threadIdx.x] = r_limit;
-        }
-    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (rt0 + i < n_tiles) fetch(rt0 + i, i);
     loaded(kf);
     loaded(vf);
-    if (rt0 < n_tiles) {
-        fetch(rt0, lds0);
-        keep(info[0]);
-    }
-    for (int rt = rt0; rt < n_tiles; ++rt) {
-        loads_landed();
-        const int at = (rt - rt0) & 1;
-        const unsigned char* tq = lds + at * 2 * BYTES;
+    int at = 0;
+    for (int rt = rt0; rt < n_tiles; ++rt, at = at + 1 == STAGES ? 0 : at + 1) {
+        tile_landed<STAGES, G::LPS>(n_tiles - 1 - rt);
+        if (rt + STAGES - 1 < n_tiles) fetch(rt + STAGES - 1, at == 0 ? STAGES - 1 : at - 1);
+        const unsigned char* tq = lds + at * G::STAGE;
         const unsigned char* tg = tq + BYTES;
-        const RowInfo& in = info[at];
-        const bool more = rt + 1 < n_tiles;
-        if (more) fetch(rt + 1, lds0 + (at ^ 1) * 2 * BYTES);
+        const float* in_lse = reinterpret_cast<const float*>(tg + BYTES) + rw * 32;
+        const float* in_delta = in_lse + 64;
         const int b0 = rt * TQ + rw * 32;
         // the block's last row sees most
         const int last_limit = min(min(b0 + 31, rows - 1) / group + shift, s.lk - 1), first_limit = min(b0 / group + shift, s.lk - 1);
@@ -702,11 +765,14 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) seen |= key <= in.limit[rw * 32 + 8 * g + 4 * half + j] ? 1u << (4 * g + j) : 0u;
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = b0 + 8 * g + 4 * half + j;
+                        seen |= r < rows && key <= min(r / group + shift, s.lk - 1) ? 1u << (4 * g + j) : 0u;
+                    }
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(&in.lse[rw * 32 + 8 * g + 4 * half]), dl = *reinterpret_cast<const f32x4*>(&in.delta[rw * 32 + 8 * g + 4 * half]);
+                const f32x4 l = *reinterpret_cast<const f32x4*>(in_lse + 8 * g + 4 * half), dl = *reinterpret_cast<const f32x4*>(in_delta + 8 * g + 4 * half);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * g + j;
@@ -724,7 +790,6 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
             add_product<E, DP, false>(av, tg, rw * 32, sc, cut, seen, lane);
             add_product<E, DP, true>(ak, tq, rw * 32, dp, cut, seen, lane);
         }
-        if (more) keep(info[at ^ 1]);
     }
     if constexpr (RW > 1) {
         float* const other = reinterpret_cast<float*>(lds) + kw * (RW - 1) * DP * 64 + lane;
@@ -787,51 +852,54 @@ Deal deal_of(int n_seqs, int total_q, int total_k, int heads, int kv_heads)
     return d;
 }
 
-template <typename E, int DP, int RW, int KW, int UB>
+template <typename E, int DP, int RW, int KW, int UB, int STAGES>
 hipError_t forward_with(const PackedAttn& p, const Deal& d, hipStream_t stream)
 {
-    using F = Forward<E, DP, RW, KW, UB>;
+    using F = Forward<E, DP, RW, KW, UB, STAGES>;
     static std::atomic<uint64_t> done{0};
-    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, RW, KW, UB>), F::LDS, done);
+    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, RW, KW, UB, STAGES>), F::LDS, done);
     if (e != hipSuccess) return e;
     if (d.items > 0x7FFFFFFF) return hipErrorInvalidValue;
-    packed_forward_kernel<E, DP, RW, KW, UB><<<dim3((unsigned)d.items, (unsigned)p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
+    packed_forward_kernel<E, DP, RW, KW, UB, STAGES><<<dim3((unsigned)d.items, (unsigned)p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
     if ((e = hipGetLastError()) != hipSuccess || d.keys_each == 0) return e;
     const int rows = std::min<int64_t>(F::BM, (int64_t)p.total_q * (p.heads / p.kv_heads));
     packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)d.tiles, (unsigned)p.kv_heads, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each);
     return hipGetLastError();
 }
+// (rings of at most 64 KB, of which a compute unit holds two, as long as that leaves two stages)
 template <typename E, int DP>
 hipError_t forward_of(const PackedAttn& p, hipStream_t stream)
 {
     const Deal d = deal_of(p.n_seqs, p.total_q, p.total_k, p.heads, p.kv_heads);
-    constexpr bool WIDE = Tile<E, DP>::ROWB == 512;         // float32, 128 columns: half the keys a tile
-    if (d.rows_each == 32) return forward_with<E, DP, 1, WIDE ? 2 : 4, 1>(p, d, stream);
-    if (d.rows_each == 64) return forward_with<E, DP, 2, 2, E::SIZE == 2 && DP == 64 ? 2 : 1>(p, d, stream);
-    return forward_with<E, DP, 4, 1, 2>(p, d, stream);
+    constexpr int ROWB = Tile<E, DP>::ROWB;
+    if (d.rows_each == 32) {
+        if constexpr (ROWB == 128) return forward_with<E, DP, 1, 4, 1, 2>(p, d, stream);
+        else return forward_with<E, DP, 1, 2, 1, 2>(p, d, stream);
+    }
+    if (d.rows_each == 64) return forward_with<E, DP, 2, 2, 1, ROWB == 128 ? 3 : 2>(p, d, stream);
+    return forward_with<E, DP, 4, 1, 2, ROWB == 128 ? 3 : 2>(p, d, stream);
 }
 
 template <typename E, int DP>
-hipError_t gradient_with(const PackedAttn& p, hipStream_t stream)
+hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
 {
-    constexpr int NW = 4;
+    constexpr int ROWB = Tile<E, DP>::ROWB, SQ = ROWB == 128 ? 3 : 2, SK = ROWB == 512 ? 2 : 3;
+    using G = KeyGrad<E, DP, 2, 2, SK>;
+    using R = RowGrad<E, DP, 2, 2, SQ>;
     static std::atomic<uint64_t> done_q{0}, done_k{0};
-    using G = KeyGrad<E, DP, 2, 2>;
-    const int bytes = 4 * 32 * Tile<E, DP>::ROWB;
-    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, NW>), bytes, done_q);
+    hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, 2, 2, SQ>), R::LDS, done_q);
     if (e != hipSuccess) return e;
-    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, 2, 2>), G::LDS, done_k);
+    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, 2, 2, SK>), G::LDS, done_k);
     if (e != hipSuccess) return e;
     float* stat = static_cast<float*>(p.work);
     const int64_t n = (int64_t)p.total_q * p.heads;
-    const int64_t tiles_q = ((int64_t)p.total_q * (p.heads / p.kv_heads) + NW * 32 - 1) / (NW * 32) + p.n_seqs;
-    const int64_t tiles_k = ((int64_t)p.total_k + G::BN - 1) / G::BN + p.n_seqs;
+    const int64_t tiles_q = (int64_t)p.total_q * (p.heads / p.kv_heads) / R::BM + p.n_seqs, tiles_k = (int64_t)p.total_k / G::BN + p.n_seqs;
     if (tiles_q > 0x7FFFFFFF || tiles_k > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
     packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dkv_kernel<E, DP, 2, 2><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
+    packed_dkv_kernel<E, DP, 2, 2, SK><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dq_kernel<E, DP, NW><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), NW * 64, bytes, stream>>>(p, stat);
+    packed_dq_kernel<E, DP, 2, 2, SQ><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), R::NW * 64, R::LDS, stream>>>(p, stat);
     return hipGetLastError();
 }
 
@@ -852,8 +920,8 @@ hipError_t launch_packed_attention(const PackedAttn& p, int f32, hipStream_t str
 
 hipError_t launch_packed_attention_grad(const PackedAttn& p, int f32, hipStream_t stream)
 {
-    if (f32) return p.d <= 64 ? gradient_with<F32, 64>(p, stream) : gradient_with<F32, 128>(p, stream);
-    return p.d <= 64 ? gradient_with<B16, 64>(p, stream) : gradient_with<B16, 128>(p, stream);
+    if (f32) return p.d <= 64 ? gradient_of<F32, 64>(p, stream) : gradient_of<F32, 128>(p, stream);
+    return p.d <= 64 ? gradient_of<B16, 64>(p, stream) : gradient_of<B16, 128>(p, stream);
 }
 
 }  // namespace mt

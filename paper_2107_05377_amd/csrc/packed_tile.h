@@ -23,6 +23,11 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0");
 }
+// the same with 4 bytes a lane
+__device__ __forceinline__ void load_to_lds_4(const void* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0");
+}
 #pragma clang diagnostic pop
 
 // ---- element types: what 16 bytes of a row mean to the matrix instructions
