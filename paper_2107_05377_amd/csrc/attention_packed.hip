@@ -43,104 +43,87 @@ __device__ __forceinline__ f32x4 acc_frag(const f32x16& s, int c, F32)
 }
 
 // ---- non-finite operands of a block that a mask cuts
-// 0 where the element is finite, else a code: +inf 1, -inf 64, NaN 4096; sums of up to 32 codes are exact and tell which were among them
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ bool split_bad(bf16x8& f, bf16x8& code)
+template <typename E>
+__device__ __forceinline__ bool any_bad(const typename E::frag& f)
 {
-    bool bad = false;
-    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-    u16x8 v = __builtin_bit_cast(u16x8, f);
+    constexpr uint32_t FULL = E::SIZE == 2 ? 0x7F807F80u : 0x7F800000u, CARRY = E::SIZE == 2 ? 0x00800080u : 0x00800000u, SIGN = E::SIZE == 2 ? 0x80008000u : 0x80000000u;
+    const u32x4 v = __builtin_bit_cast(u32x4, f);       // (of the whole vector: a bit cast of one element reads element 0)
+    uint32_t t = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const bool b = (v[j] & 0x7F80) == 0x7F80;
-        code[j] = !b ? (__bf16)0.f : (v[j] & 0x7F) ? (__bf16)4096.f : (v[j] & 0x8000) ? (__bf16)64.f : (__bf16)1.f;
-        v[j] = b ? 0 : v[j];
-        bad |= b;
-    }
-    f = __builtin_bit_cast(bf16x8, v);
-    return bad;
+    for (int j = 0; j < 4; ++j) t |= (v[j] & FULL) + CARRY;         // a full exponent carries into the sign's place
+    return (t & SIGN) != 0;
 }
-__device__ __forceinline__ bool split_bad(f32x4& f, f32x4& code)
+// non-finite elements replaced by 0
+template <typename E>
+__device__ __forceinline__ void drop_bad(typename E::frag& f)
 {
-    bool bad = false;
-    u32x4 v = __builtin_bit_cast(u32x4, f);          // (of the whole vector: a bit cast of one element reads element 0)
+    u32x4 v = __builtin_bit_cast(u32x4, f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const bool b = (v[j] & 0x7F800000u) == 0x7F800000u;
-        code[j] = !b ? 0.f : (v[j] & 0x7FFFFFu) ? 4096.f : (v[j] >> 31) ? 64.f : 1.f;
-        v[j] = b ? 0u : v[j];
-        bad |= b;
+        if constexpr (E::SIZE == 2) {
+            const uint32_t t = (v[j] & 0x7F807F80u) + 0x00800080u;
+            v[j] &= ((t & 0x8000u) ? 0u : 0xFFFFu) | ((t >> 31) ? 0u : 0xFFFF0000u);
+        } else v[j] = ((v[j] & 0x7F800000u) + 0x00800000u) >> 31 ? 0u : v[j];
     }
-    f = __builtin_bit_cast(f32x4, v);
-    return bad;
-}
-__device__ __forceinline__ bool any_bad(const bf16x8& f)
-{
-    const u32x4 v = __builtin_bit_cast(u32x4, f);
-    uint32_t t = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) t |= (v[j] & 0x7F807F80u) + 0x00800080u;       // a full exponent carries into the sign's place
-    return (t & 0x80008000u) != 0;
-}
-__device__ __forceinline__ bool any_bad(const f32x4& f)
-{
-    const u32x4 v = __builtin_bit_cast(u32x4, f);
-    uint32_t t = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) t |= (v[j] & 0x7F800000u) + 0x00800000u;
-    return (t >> 31) != 0;
+    f = __builtin_bit_cast(typename E::frag, v);
 }
 
-// acc += (columns of the tile) x w, w the accumulators of a block of 32 rows (in the sum) whose element i is nonzero only where bit i of `seen`
-// is set; `cut`: some are not set.  w carries a sign (dS) or not (P): an infinity is put back with its own sign only for P, as NaN for dS.
-template <typename E, int DP, bool SIGNED>
-__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsigned char* t, int row0, const f32x16& w, bool cut, uint32_t seen, int lane)
+// acc += (columns of the tile) x w, w the accumulators of a block of 32 rows (of the sum), 0 in row k of a lane that does not see it (sees(k)); `cut`:
+// there are such.  What is not seen must not reach the result, but 0 times a non-finite operand is NaN: where a cut block's operands hold such
+// (which a few instructions tell), they are taken out, and put back one by one for the lanes that see them.  w carries a sign (dS) or not (P):
+// an infinity is put back with its own sign only for P, as NaN for dS.
+template <typename E, int DP, bool SIGNED, typename Sees>
+__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsigned char* t, int row0, const f32x16& w, bool cut, Sees sees, int lane)
 {
     using T = Tile<E, DP>;
     constexpr int STEPS = 32 / E::KS;
     typename E::frag wf[STEPS];
 #pragma unroll
     for (int c = 0; c < STEPS; ++c) wf[c] = acc_frag(w, c, E{});
-    if (!cut) {
+    // 64 columns at a time: their operands are read at once, and there is one branch for the rare case
 #pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
+    for (int d0 = 0; d0 < DP / 32; d0 += 2) {
+        typename E::frag a[2][STEPS];
 #pragma unroll
-            for (int c = 0; c < STEPS; ++c) acc[db] = E::mma(T::col_frag(t, row0, db, c, lane), wf[c], acc[db]);
-        return;
-    }
+        for (int db = 0; db < 2; ++db)
 #pragma unroll
-    for (int db = 0; db < DP / 32; ++db) {
-        typename E::frag a[STEPS];
-        bool bad = false;
+            for (int c = 0; c < STEPS; ++c) a[db][c] = T::col_frag(t, row0, d0 + db, c, lane);
+        if (cut) {
+            bool bad = false;
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) {
-            a[c] = T::col_frag(t, row0, db, c, lane);
-            bad |= any_bad(a[c]);
-        }
-        if (__any(bad)) {
-            f32x16 code;
+            for (int db = 0; db < 2; ++db)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) code[i] = 0.f;
+                for (int c = 0; c < STEPS; ++c) bad |= any_bad<E>(a[db][c]);
+            if (__any(bad)) {
 #pragma unroll
-            for (int c = 0; c < STEPS; ++c) {
-                typename E::frag m, one;
-                split_bad(a[c], m);
-                f32x16 s;
+                for (int db = 0; db < 2; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = (seen >> i) & 1 ? 1.f : 0.f;
-                one = acc_frag(s, c, E{});
-                code = E::mma(m, one, code);
+                    for (int c = 0; c < STEPS; ++c) drop_bad<E>(a[db][c]);
+#pragma unroll 1
+                for (int k = 0; k < 32; ++k) {
+                    const int r = row0 + k, at = (d0 * 32 + lane) * E::SIZE;       // a lane reads one of the 64 columns of row k
+                    const unsigned char* e = t + r * T::ROWB + (((at >> 4) ^ T::key(r)) << 4) + (at & 15);
+                    const uint32_t v = E::SIZE == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(e) << 16 : *reinterpret_cast<const uint32_t*>(e);
+                    uint64_t m = __ballot((v & 0x7F800000u) == 0x7F800000u);
+                    const bool mine = sees(k);
+                    while (m) {
+                        const int col = __ffsll((unsigned long long)m) - 1, i_at = (col >> 5) * 16 + ((col >> 3) & 3) * 4 + (col & 3);
+                        m &= m - 1;
+                        float put = __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)v, col));
+                        put = SIGNED ? NAN : put;
+                        put = mine && (lane >> 5) == ((col >> 2) & 1) ? put : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == i_at) acc[d0 + (i >> 4)][i & 15] += put;
+                    }
+                }
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int n = (int)code[i];
-                const bool up = (n & 63) != 0, down = (n & 4032) != 0;
-                const float put = (SIGNED || n >= 4096 || (up && down)) ? NAN : up ? INFINITY : -INFINITY;
-                acc[db][i] += n ? put : 0.f;
-            }
         }
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) acc[db] = E::mma(a[c], wf[c], acc[db]);
+        for (int c = 0; c < STEPS; ++c)
+#pragma unroll
+            for (int db = 0; db < 2; ++db) acc[d0 + db] = E::mma(a[db][c], wf[c], acc[d0 + db]);
     }
 }
 
@@ -165,9 +148,9 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
     int base = 0, base_items = 0;
     for (int b0 = 0; b0 < p.n_seqs; b0 += 64 * NW) {
         const bool one = p.n_seqs - b0 <= 64;               // every wavefront looks at the same sequences: nothing to exchange
-        const int at = b0 + (one ? lane : (int)threadIdx.x), b = min(at, p.n_seqs - 1);
+        const int mine_b = b0 + (one ? lane : (int)threadIdx.x), b = min(mine_b, p.n_seqs - 1);
         const int a = clamp_start(start[b], total), e = clamp_start(start[b + 1], total);
-        const int tiles = at < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
+        const int tiles = mine_b < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
         int chunks = 1;
         if (keys_each > 0) chunks = max(1, (max(clamp_start(p.k_start[b + 1], p.total_k) - clamp_start(p.k_start[b], p.total_k), 0) + keys_each - 1) / keys_each);
         const int n = BY_TILE ? tiles : tiles * chunks;
@@ -211,7 +194,7 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
                 first_items = base_items + __shfl(items, l) - tiles_n * s.chunks;
             } else {
                 if (w >= base + sum - n && w < base + sum) {
-                    found[0] = at;
+                    found[0] = mine_b;
                     found[1] = w - (base + sum - n);
                     found[2] = chunks;
                     found[3] = base_items + items - tiles * chunks;
@@ -222,13 +205,18 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
                 s.chunks = found[2];
                 first_items = found[3];
             }
+            // (the same in all lanes, which the compiler is told: what is reckoned from them is scalar work)
+            seq = __builtin_amdgcn_readfirstlane(seq);
+            mine = __builtin_amdgcn_readfirstlane(mine);
+            s.chunks = __builtin_amdgcn_readfirstlane(s.chunks);
             s.tile = BY_TILE ? mine : mine / s.chunks;
             s.chunk = BY_TILE ? 0 : mine - s.tile * s.chunks;
-            s.first = BY_TILE ? first_items + s.tile * s.chunks : w - s.chunk;
-            s.q0 = clamp_start(p.q_start[seq], p.total_q);
-            s.lq = max(clamp_start(p.q_start[seq + 1], p.total_q) - s.q0, 0);
-            s.k0 = clamp_start(p.k_start[seq], p.total_k);
-            s.lk = max(clamp_start(p.k_start[seq + 1], p.total_k) - s.k0, 0);
+            s.first = BY_TILE ? __builtin_amdgcn_readfirstlane(first_items) + s.tile * s.chunks : w - s.chunk;
+            const auto at = [](const int32_t* start, int i, int total) { return __builtin_amdgcn_readfirstlane(clamp_start(start[i], total)); };
+            s.q0 = at(p.q_start, seq, p.total_q);
+            s.lq = max(at(p.q_start, seq + 1, p.total_q) - s.q0, 0);
+            s.k0 = at(p.k_start, seq, p.total_k);
+            s.lk = max(at(p.k_start, seq + 1, p.total_k) - s.k0, 0);
             return true;
         }
         base += all;
@@ -238,30 +226,60 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
     return false;
 }
 
-// rows row0 .. row0 + ROWS - 1 (none beyond `last`, whose copy stands in) of a matrix into an LDS tile, 16 bytes a lane straight from memory.
+// A matrix whose tiles of ROWS rows go into LDS, 16 bytes a lane straight from memory.  Row r is row r / group of its head r % group.  A lane's place inside
+// a tile is an offset that stays the same from tile to tile (32 bits, from the tile's first row on: where a tile is whole tokens and spans less than
+// 4 GB), so a whole tile costs scalar instructions only; the last tile, beyond whose rows copies of the last one stand in, is reckoned out.
 // Columns beyond the head's width hold copies of the first ones: they meet zeros, or results that nobody stores.
-template <typename E, int DP, int ROWS, int NW, bool GROUPED>
-__device__ __forceinline__ void stage(const typename E::elem* base, int64_t row_stride, int64_t head_stride, int group, int row0, int last, int d, uint32_t t)
-{
+template <typename E, int DP, int ROWS, int NW>
+struct Rows {
     using T = Tile<E, DP>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int N = ROWS / T::RPI;
-    static_assert(N % NW == 0, "rows must split evenly over wavefront loads");
-#pragma unroll
-    for (int i = 0; i < N / NW; ++i) {
-        const int blk = __builtin_amdgcn_readfirstlane(wave + i * NW);
-        const int row = blk * T::RPI + lane / T::CH;
-        int chunk = (lane % T::CH) ^ T::key(row);
-        if (chunk * E::EPC >= d) chunk = 0;
-        const int r = min(row0 + row, last);
-        const typename E::elem* at;
-        if constexpr (GROUPED) {
-            const int tok = r / group;
-            at = base + tok * row_stride + (r - tok * group) * head_stride;
-        } else at = base + r * row_stride;
-        load_to_lds(at + chunk * E::EPC, t + blk * 1024);
+    static constexpr int N = ROWS / T::RPI / NW;
+    static_assert(N * NW * T::RPI == ROWS, "rows must split evenly over wavefront loads");
+    const char* base;
+    int64_t row_bytes, head_bytes, step;
+    uint32_t off[N];
+    int group, d;
+    bool even;
+
+    __device__ __forceinline__ uint32_t column(int row) const
+    {
+        const int lane = threadIdx.x & 63;
+        const int chunk = (lane % T::CH) ^ T::key(row);
+        return chunk * E::EPC >= d ? 0 : chunk * 16;
     }
-}
+    __device__ __forceinline__ void init(const typename E::elem* from, int64_t row, int64_t head, int group_, int d_)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        base = reinterpret_cast<const char*>(from);
+        row_bytes = row * E::SIZE;
+        head_bytes = head * E::SIZE;
+        group = group_;
+        d = d_;
+        step = ROWS / group * row_bytes;
+        even = ROWS % group == 0 && step + group * head_bytes < (1ll << 32);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = (wave + i * NW) * T::RPI + lane / T::CH, tok = r / group;
+            off[i] = (uint32_t)(tok * row_bytes + (r - tok * group) * head_bytes) + column(r);
+        }
+    }
+    __device__ __forceinline__ void fetch(int tile, int last, uint32_t to) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (even && (tile + 1) * ROWS - 1 <= last) {
+            const char* at = uniform(base + tile * step);
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_to_lds(at, off[i], to + (wave + i * NW) * 1024);
+            return;
+        }
+        const int lane = threadIdx.x & 63;
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+            const int in = (wave + i * NW) * T::RPI + lane / T::CH, r = min(tile * ROWS + in, last), tok = r / group;
+            load_to_lds(base + tok * row_bytes + (r - tok * group) * head_bytes + column(in), to + (wave + i * NW) * 1024);
+        }
+    }
+};
 
 // The tiles that pass by go through a ring in LDS: one is used while up to STAGES - 1 are under way.  All loads of a loop are those of its ring, LPS of each
 // wavefront per tile, so that a wait can leave the last tiles under way.
@@ -329,7 +347,7 @@ struct Forward {
 };
 
 template <typename E, int DP, int RW, int KW, int UB, int STAGES>
-__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_forward_kernel(PackedAttn p, int keys_each)
+__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 && UB == 1 ? 3 : 2) : 1)) void packed_forward_kernel(PackedAttn p, int keys_each)
 {
     using F = Forward<E, DP, RW, KW, UB, STAGES>;
     using T = Tile<E, DP>;
@@ -358,10 +376,13 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_f
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    Rows<E, DP, TK, NW> rows_k, rows_v;
+    rows_k.init(K, p.k_row, 0, 1, p.d);
+    rows_v.init(V, p.v_row, 0, 1, p.d);
     const auto fetch = [&](int kt, int stage_at) {
         const uint32_t to = lds0 + stage_at * 2 * BYTES;
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, kt * TK, s.lk - 1, p.d, to);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, kt * TK, s.lk - 1, p.d, to + BYTES);
+        rows_k.fetch(kt, s.lk - 1, to);
+        rows_v.fetch(kt, s.lk - 1, to + BYTES);
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
@@ -395,18 +416,11 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_f
             for (int ks = 0; ks < DP / E::KS; ++ks) sc[u] = E::mma(T::row_frag(tk, u * 32 + l32, ks, half), qf[ks], sc[u]);
         }
         const bool cut = key0 + UB * 32 - 1 > wave_min;
-        uint32_t seen[UB];
         if (cut) {
 #pragma unroll
-            for (int u = 0; u < UB; ++u) {
-                seen[u] = 0;
+            for (int u = 0; u < UB; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool see = key0 + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit;
-                    seen[u] |= see ? 1u << i : 0u;
-                    sc[u][i] = see ? sc[u][i] : -INFINITY;
-                }
-            }
+                for (int i = 0; i < 16; ++i) sc[u][i] = key0 + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? sc[u][i] : -INFINITY;
         }
         float top = sc[0][0];
 #pragma unroll
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_f
                 sum += sc[u][i];
             }
 #pragma unroll
-        for (int u = 0; u < UB; ++u) add_product<E, DP, false>(acc, tv, u * 32, sc[u], cut, seen[u], lane);
+        for (int u = 0; u < UB; ++u) add_product<E, DP, false>(acc, tv, u * 32, sc[u], cut, [&](int k) { return key0 + u * 32 + k <= limit; }, lane);
     }
     sum = lane_pair_sum<32>(sum);
     if constexpr (KW > 1) {
@@ -579,7 +593,7 @@ struct RowGrad {
 };
 
 template <typename E, int DP, int RW, int KW, int STAGES>
-__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
+__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
 {
     using R = RowGrad<E, DP, RW, KW, STAGES>;
     using T = Tile<E, DP>;
@@ -603,10 +617,13 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_d
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
+    Rows<E, DP, TK, NW> rows_k, rows_v;
+    rows_k.init(K, p.k_row, 0, 1, p.d);
+    rows_v.init(V, p.v_row, 0, 1, p.d);
     const auto fetch = [&](int kt, int stage_at) {
         const uint32_t to = lds0 + stage_at * 2 * BYTES;
-        stage<E, DP, TK, NW, false>(K, p.k_row, 0, 1, kt * TK, s.lk - 1, p.d, to);
-        stage<E, DP, TK, NW, false>(V, p.v_row, 0, 1, kt * TK, s.lk - 1, p.d, to + BYTES);
+        rows_k.fetch(kt, s.lk - 1, to);
+        rows_v.fetch(kt, s.lk - 1, to + BYTES);
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
@@ -643,19 +660,13 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? 2 : 1)) void packed_d
             dp = E::mma(T::row_frag(tv, kw * 32 + l32, ks, half), gf[ks], dp);
         }
         const bool cut = key0 + 31 > wave_min;
-        uint32_t seen = 0xFFFFu;
-        if (cut) {
-            seen = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) seen |= key0 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? 1u << i : 0u;
-        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
         if (cut) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = (seen >> i) & 1 ? sc[i] : 0.f;
+            for (int i = 0; i < 16; ++i) sc[i] = key0 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? sc[i] : 0.f;
         }
-        add_product<E, DP, true>(acc, tk, kw * 32, sc, cut, seen, lane);
+        add_product<E, DP, true>(acc, tk, kw * 32, sc, cut, [&](int k) { return key0 + k <= limit; }, lane);
     }
     if constexpr (KW > 1) {
         float* const other = reinterpret_cast<float*>(lds) + rw * (KW - 1) * DP / 2 * 64 + lane;
@@ -708,9 +719,10 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;
     const int my_key = n0 + kw * 32 + l32, key = min(my_key, s.lk - 1);
     const int wave_last = min(n0 + kw * 32 + 31, s.lk - 1), wave_first = n0 + kw * 32;
-    // the first query that sees the tile's first key
-    const int t_first = p.causal ? min(max(n0 - shift, 0), s.lq) : 0;
-    const int rt0 = t_first * group / TQ, n_tiles = (rows + TQ - 1) / TQ;
+    // the first rows that see the wavefront's first key, all its keys, the lane's key
+    const auto first_of = [&](int k) { return p.causal ? min(max(k - shift, 0), s.lq) * group : 0; };
+    const int row_first = first_of(wave_first), row_all = first_of(wave_last), my_first = first_of(key);
+    const int rt0 = first_of(n0) / TQ, n_tiles = (rows + TQ - 1) / TQ;
 
     typename E::frag kf[DP / E::KS], vf[DP / E::KS];
     load_row<E, DP>(kf, static_cast<const elem*>(p.k) + (int64_t)(s.k0 + key) * p.k_row + kvh * p.k_head, p.d, half);
@@ -727,10 +739,13 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
 
     // wavefronts 0, 2 .. fetch lse, 1, 3 .. delta
     const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group + (wave & 1) * (int64_t)p.total_q * p.heads;
+    Rows<E, DP, TQ, NW> rows_q, rows_g;
+    rows_q.init(Q, p.q_row, p.q_head, group, p.d);
+    rows_g.init(O, p.g_row, p.g_head, group, p.d);
     const auto fetch = [&](int rt, int stage_at) {
         const uint32_t to = lds0 + stage_at * G::STAGE;
-        stage<E, DP, TQ, NW, true>(Q, p.q_row, p.q_head, group, rt * TQ, rows - 1, p.d, to);
-        stage<E, DP, TQ, NW, true>(O, p.g_row, p.g_head, group, rt * TQ, rows - 1, p.d, to + BYTES);
+        rows_q.fetch(rt, rows - 1, to);
+        rows_g.fetch(rt, rows - 1, to + BYTES);
         load_to_lds_4(my_stat + min(rt * TQ + lane, rows - 1), to + 2 * BYTES + wave * 256);
     };
 #pragma unroll
@@ -747,9 +762,7 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
         const float* in_lse = reinterpret_cast<const float*>(tg + BYTES) + rw * 32;
         const float* in_delta = in_lse + 64;
         const int b0 = rt * TQ + rw * 32;
-        // the block's last row sees most
-        const int last_limit = min(min(b0 + 31, rows - 1) / group + shift, s.lk - 1), first_limit = min(b0 / group + shift, s.lk - 1);
-        if (b0 < rows && wave_first <= last_limit) {
+        if (b0 < rows && b0 + 31 >= row_first) {
             f32x16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
@@ -758,18 +771,8 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
                 sc = E::mma(T::row_frag(tq, rw * 32 + l32, ks, half), kf[ks], sc);
                 dp = E::mma(T::row_frag(tg, rw * 32 + l32, ks, half), vf[ks], dp);
             }
-            const bool cut = wave_last > first_limit || b0 + 32 > rows;
-            uint32_t seen = 0xFFFFu;
-            if (cut) {
-                seen = 0;
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int r = b0 + 8 * g + 4 * half + j;
-                        seen |= r < rows && key <= min(r / group + shift, s.lk - 1) ? 1u << (4 * g + j) : 0u;
-                    }
-            }
+            const bool cut = b0 < row_all || b0 + 32 > rows;
+            const auto sees = [&](int k) { return b0 + k >= my_first && b0 + k < rows; };
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 l = *reinterpret_cast<const f32x4*>(in_lse + 8 * g + 4 * half), dl = *reinterpret_cast<const f32x4*>(in_delta + 8 * g + 4 * half);
@@ -783,12 +786,13 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
             if (cut) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    sc[i] = (seen >> i) & 1 ? sc[i] : 0.f;
-                    dp[i] = (seen >> i) & 1 ? dp[i] : 0.f;
+                    const bool see = sees(8 * (i >> 2) + 4 * half + (i & 3));
+                    sc[i] = see ? sc[i] : 0.f;
+                    dp[i] = see ? dp[i] : 0.f;
                 }
             }
-            add_product<E, DP, false>(av, tg, rw * 32, sc, cut, seen, lane);
-            add_product<E, DP, true>(ak, tq, rw * 32, dp, cut, seen, lane);
+            add_product<E, DP, false>(av, tg, rw * 32, sc, cut, sees, lane);
+            add_product<E, DP, true>(ak, tq, rw * 32, dp, cut, sees, lane);
         }
     }
     if constexpr (RW > 1) {

@@ -23,6 +23,17 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0");
 }
+// a pointer that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p)
+{
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    return reinterpret_cast<const char*>((uintptr_t)((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v)));
+}
+// the same from a place that all lanes share and a lane's offset in bytes
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base) : "m0");
+}
 // the same with 4 bytes a lane
 __device__ __forceinline__ void load_to_lds_4(const void* from, uint32_t to)
 {
