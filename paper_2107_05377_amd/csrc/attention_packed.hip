@@ -134,6 +134,8 @@ struct Seq {
 };
 __device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v, 0), total); }
 
+// Workgroups: key heads first, so that the tiles of a sequence, whose cost falls from the first to the last, end a launch with the cheapest, and a key head's
+// workgroups share an XCD where there are 8 key heads or a part of 8.
 // Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with
 // keys_each > 0 its sequence's chunks of that many keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are
 // brought inside, a sequence that would end before it starts is empty.  A workgroup looks through 64 sequences for each of its wavefronts at a time:
@@ -355,9 +357,9 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 && UB == 1 
     constexpr int BM = F::BM, TK = F::TK, NW = F::NW, BYTES = F::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // the ring of keys and values
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
-    if (!find_tile<NW, false>(p, blockIdx.x, group, BM, keys_each, s)) return;
+    if (!find_tile<NW, false>(p, item, group, BM, keys_each, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
@@ -514,11 +516,11 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys
 {
     typedef typename E::elem elem;
     constexpr int ROW = DP + 4, COLS = DP / 64;
-    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
-    if (!find_tile<4, false, true>(p, blockIdx.x, group, BM, keys_each, s) || s.chunks == 1) return;
+    if (!find_tile<4, false, true>(p, item, group, BM, keys_each, s) || s.chunks == 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r = blockIdx.z * 4 + wave, row = (tiles - 1 - s.tile) * BM + r;
+    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r = blockIdx.y * 4 + wave, row = (tiles - 1 - s.tile) * BM + r;
     if (row >= rows) return;
     const int tok = row / group, head = kvh * group + row - tok * group;
     const int limit = min(tok + (p.causal ? s.lk - s.lq : 0x40000000), s.lk - 1);
@@ -601,9 +603,9 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
     constexpr int BM = R::BM, TK = R::TK, NW = R::NW, BYTES = R::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
-    if (!find_tile<NW, false>(p, blockIdx.x, group, BM, 0, s)) return;
+    if (!find_tile<NW, false>(p, item, group, BM, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
@@ -710,9 +712,9 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
     constexpr int BN = G::BN, TQ = G::TQ, NW = G::NW, BYTES = G::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, kvh = blockIdx.y;
+    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
-    if (!find_tile<NW, true>(p, blockIdx.x, 1, BN, 0, s)) return;
+    if (!find_tile<NW, true>(p, item, 1, BN, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int kw = wave / RW, rw = wave % RW;
     const int rows = s.lq * group, n0 = s.tile * BN;
@@ -863,11 +865,11 @@ hipError_t forward_with(const PackedAttn& p, const Deal& d, hipStream_t stream)
     static std::atomic<uint64_t> done{0};
     hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, RW, KW, UB, STAGES>), F::LDS, done);
     if (e != hipSuccess) return e;
-    if (d.items > 0x7FFFFFFF) return hipErrorInvalidValue;
-    packed_forward_kernel<E, DP, RW, KW, UB, STAGES><<<dim3((unsigned)d.items, (unsigned)p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
+    if (d.items * p.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    packed_forward_kernel<E, DP, RW, KW, UB, STAGES><<<(unsigned)(d.items * p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
     if ((e = hipGetLastError()) != hipSuccess || d.keys_each == 0) return e;
     const int rows = std::min<int64_t>(F::BM, (int64_t)p.total_q * (p.heads / p.kv_heads));
-    packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)d.tiles, (unsigned)p.kv_heads, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each);
+    packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)(d.tiles * p.kv_heads), (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each);
     return hipGetLastError();
 }
 // (rings of at most 64 KB, of which a compute unit holds two, as long as that leaves two stages)
@@ -898,12 +900,12 @@ hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
     float* stat = static_cast<float*>(p.work);
     const int64_t n = (int64_t)p.total_q * p.heads;
     const int64_t tiles_q = (int64_t)p.total_q * (p.heads / p.kv_heads) / R::BM + p.n_seqs, tiles_k = (int64_t)p.total_k / G::BN + p.n_seqs;
-    if (tiles_q > 0x7FFFFFFF || tiles_k > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (tiles_q * p.kv_heads > 0x7FFFFFFF || tiles_k * p.kv_heads > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
     packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dkv_kernel<E, DP, 2, 2, SK><<<dim3((unsigned)tiles_k, (unsigned)p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
+    packed_dkv_kernel<E, DP, 2, 2, SK><<<(unsigned)(tiles_k * p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dq_kernel<E, DP, 2, 2, SQ><<<dim3((unsigned)tiles_q, (unsigned)p.kv_heads), R::NW * 64, R::LDS, stream>>>(p, stat);
+    packed_dq_kernel<E, DP, 2, 2, SQ><<<(unsigned)(tiles_q * p.kv_heads), R::NW * 64, R::LDS, stream>>>(p, stat);
     return hipGetLastError();
 }
 
