@@ -123,8 +123,8 @@ def lib():
         L.mt_op_panel_layernorm.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, i32, vp, i32, i32, vp]
         L.mt_op_linear_sub.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, i32, i32, i64, i64, i64, i64, vp, vp, i32, vp]
         L.mt_debug_set_gemm_tile.restype = i32
-        L.mt_op_packed_attention.argtypes = L.mt_op_packed_attention_grad.argtypes = [C.POINTER(mt_packed_attention), vp]
-        L.mt_op_packed_attention_work.argtypes = [C.POINTER(mt_packed_attention), i32]
+        L.mt_op_packed_attention.argtypes = L.mt_op_packed_attention_grad.argtypes = [vp, vp]      # (the struct by reference, or its packed bytes)
+        L.mt_op_packed_attention_work.argtypes = [vp, i32]
         L.mt_op_vocab_loss.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, sz, vp]
         L.mt_op_vocab_loss_grad.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
         L.mt_op_vocab_loss_work.argtypes = [i32, i32, i32, i32, i32]
@@ -583,6 +583,9 @@ def op_layernorm(x, gamma, beta, eps, want_bf16=False):
     return (of, ob) if want_bf16 else of
 
 
+# ---- operators on packed tokens.  A call of few tokens takes the device a few microseconds, so what stands between it and the library is kept short:
+# one comparison for each thing that is checked, texts only for what is refused, the argument struct packed in one go.
+
 def _refuse(name, text, code=MT_ERR_SHAPE):
     raise MTError(code, f"{name}: {text}")
 
@@ -596,55 +599,73 @@ def _act_type(name, precision):
     return torch.float32
 
 
-def _check_tensor(name, what, t, shape, dtype, device):
-    """A tensor of `shape` (None: any) and `dtype` on the call's device, whose last dimension is contiguous."""
-    if t.device != device or device.type != "cuda":
-        _refuse(name, f"{what} is on {t.device}, the call on {device}: all tensors of a call are on one GPU")
-    if t.dtype != dtype:
+def _check(name, what, t, shape, dtype, gpu):
+    """t: `shape`, `dtype`, on GPU number `gpu` (the call's), last dimension contiguous."""
+    if t.dtype is dtype and t.get_device() == gpu and gpu >= 0 and t.shape == shape and (t.stride(-1) == 1 or shape[-1] <= 1):
+        return
+    if t.get_device() != gpu or gpu < 0:
+        _refuse(name, f"{what} is on {t.device}: all tensors of a call are on one GPU")
+    if t.dtype is not dtype:
         _refuse(name, f"{what} is {t.dtype}, not {dtype}")
-    have = tuple(t.shape)
-    if have != shape and (len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have))):
-        _refuse(name, f"{what} is {have}, not {shape}")
-    if have[-1] > 1 and t.stride(-1) != 1:
-        _refuse(name, f"the last dimension of {what} is not contiguous")
+    if t.shape != shape:
+        _refuse(name, f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+    _refuse(name, f"the last dimension of {what} is not contiguous")
 
 
-def _run(name, device, work_bytes, call):
-    """call(work pointer, work bytes, stream) with a workspace of its own, on `device` and its current stream."""
+def _dims(name, what, t, n):
+    if t.dim() != n:
+        _refuse(name, f"{what} has {t.dim()} dimensions, not {n}")
+    return t.shape
+
+
+def _run(name, gpu, work_bytes, call):
+    """call(work pointer, work bytes, stream) with a workspace of its own, on GPU `gpu` and its current stream."""
     import torch
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _run(name, device, work_bytes, call)
-    work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None
-    rc = call(work.data_ptr() if work_bytes else None, work_bytes, torch.cuda.current_stream(device).cuda_stream)
+    if gpu != torch.cuda.current_device():
+        with torch.cuda.device(gpu):
+            return _run(name, gpu, work_bytes, call)
+    work = torch.empty(work_bytes, dtype=torch.uint8, device="cuda") if work_bytes else None
+    rc = call(work.data_ptr() if work_bytes else None, work_bytes, torch._C._cuda_getCurrentRawStream(gpu))
     if rc != MT_OK:
         raise MTError(rc, name)
 
 
-def _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale):
-    dt = _act_type(name, precision)
-    if q.dim() != 3 or k.dim() != 3:
-        _refuse(name, "q, k and v are [rows][heads][width]")
-    (tq, heads, d), (tk, kv_heads, _) = q.shape, k.shape
-    _check_tensor(name, "q", q, (tq, heads, d), dt, q.device)
-    _check_tensor(name, "k", k, (tk, kv_heads, d), dt, q.device)
-    _check_tensor(name, "v", v, (tk, kv_heads, d), dt, q.device)
+_ATTENTION = struct.Struct("11Q16q8if4xQQ")           # mt_packed_attention
+assert _ATTENTION.size == C.sizeof(mt_packed_attention)
+
+
+def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, scale, ctx, lse, grads=None):
+    """The checks and the call of both attention entry points; grads: (grad_ctx, grad_q, grad_k, grad_v)."""
     import torch
-    _check_tensor(name, "q_start", q_start, (None,), torch.int32, q.device)
+    dt, gpu = _act_type(name, precision), q.get_device()
+    (tq, heads, d), (tk, kv_heads, _) = _dims(name, "q", q, 3), _dims(name, "k", k, 3)
+    n_starts = _dims(name, "q_start", q_start, 1)
+    key_shape = (tk, kv_heads, d)
+    _check(name, "q", q, q.shape, dt, gpu)
+    _check(name, "k", k, key_shape, dt, gpu)
+    _check(name, "v", v, key_shape, dt, gpu)
+    _check(name, "ctx", ctx, q.shape, dt, gpu)
+    _check(name, "q_start", q_start, n_starts, torch.int32, gpu)
     if k_start is not None:
-        _check_tensor(name, "k_start", k_start, tuple(q_start.shape), torch.int32, q.device)
-    op = mt_packed_attention(precision=precision, n_seqs=q_start.shape[0] - 1, heads=heads, kv_heads=kv_heads, width=d, total_q=tq, total_k=tk,
-                             causal=1 if causal else 0, scale=1.0 / float(d) ** 0.5 if scale is None else scale, d_q_start=q_start.data_ptr(),
-                             d_k_start=None if k_start is None else k_start.data_ptr())
-    for field, t in (("q", q), ("k", k), ("v", v)):
-        _set_rows(op, field, t)
-    return op, dt
+        _check(name, "k_start", k_start, n_starts, torch.int32, gpu)
+    if lse is not None:
+        _check(name, "lse", lse, (heads, tq), torch.float32, gpu)
+        if not lse.is_contiguous():
+            _refuse(name, "lse is not contiguous")
+    g_ptr, g_str = (0, 0, 0, 0), (0,) * 8
+    if grads is not None:
+        for what, t, like in zip(("grad_ctx", "grad_q", "grad_k", "grad_v"), grads, (q, q, k, k)):
+            _check(name, what, t, like.shape, dt, gpu)
+        g_ptr, g_str = [t.data_ptr() for t in grads], [n for t in grads for n in t.stride()[:2]]
+    (qr, qh, _), (kr, kh, _), (vr, vh, _), (cr, ch, _) = q.stride(), k.stride(), v.stride(), ctx.stride()
 
-
-def _set_rows(op, field, t):
-    setattr(op, "d_" + field, t.data_ptr())
-    setattr(op, field + "_row", t.stride(0))
-    setattr(op, field + "_head", t.stride(1))
+    def pack(work, size):
+        return _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), ctx.data_ptr(), 0 if lse is None else lse.data_ptr(), q_start.data_ptr(),
+                               0 if k_start is None else k_start.data_ptr(), *g_ptr, qr, qh, kr, kh, vr, vh, cr, ch, *g_str, precision, n_starts[0] - 1, heads,
+                               kv_heads, d, tq, tk, 1 if causal else 0, d ** -0.5 if scale is None and d > 0 else scale or 0.0, work or 0, size)
+    L = lib()
+    need = L.mt_op_packed_attention_work(pack(0, 0), 0 if grads is None else 1)
+    _run(name, gpu, need, lambda work, size, stream: getattr(L, entry)(pack(work, size), stream))
 
 
 def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, scale=None, out=None, want_lse=False):
@@ -652,65 +673,40 @@ def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, 
     [sequences + 1]; scale None: 1 / sqrt(width).  Returns the context [queries][heads][width] (`out`, or zeros where no sequence is) and with want_lse
     the statistics [heads][queries] float32 for the gradient."""
     import torch
-    name = "mt_op_packed_attention"
-    op, dt = _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale)
-    if out is None:
-        out = torch.zeros(tuple(q.shape), dtype=dt, device=q.device)
-    _check_tensor(name, "out", out, tuple(q.shape), dt, q.device)
-    _set_rows(op, "ctx", out)
-    lse = torch.full((q.shape[1], q.shape[0]), float("-inf"), dtype=torch.float32, device=q.device) if want_lse else None
-    op.d_lse = None if lse is None else lse.data_ptr()
-
-    def call(work, work_bytes, stream):
-        op.d_work, op.work_bytes = work, work_bytes
-        return lib().mt_op_packed_attention(C.byref(op), stream)
-    _run(name, q.device, lib().mt_op_packed_attention_work(C.byref(op), 0), call)
-    return (out, lse) if want_lse else out
+    ctx = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    lse = q.new_full((q.shape[1], q.shape[0]), float("-inf"), dtype=torch.float32) if want_lse else None
+    _attention_call("mt_op_packed_attention", "mt_op_packed_attention", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse)
+    return (ctx, lse) if want_lse else ctx
 
 
 def op_packed_attention_grad(precision, grad_ctx, q, k, v, ctx, lse, q_start, k_start=None, causal=True, scale=None, out=None):
     """mt_op_packed_attention_grad: the gradients of q, k and v (`out`, three tensors, or new ones with zeros where no sequence is) from grad_ctx and the
     ctx and lse of op_packed_attention with the same arguments."""
     import torch
-    name = "mt_op_packed_attention_grad"
-    op, dt = _packed_attention(name, precision, q, k, v, q_start, k_start, causal, scale)
-    _check_tensor(name, "grad_ctx", grad_ctx, tuple(q.shape), dt, q.device)
-    _check_tensor(name, "ctx", ctx, tuple(q.shape), dt, q.device)
-    _check_tensor(name, "lse", lse, (q.shape[1], q.shape[0]), torch.float32, q.device)
-    if not lse.is_contiguous():
-        _refuse(name, "lse is not contiguous")
     if out is None:
-        out = tuple(torch.zeros(tuple(t.shape), dtype=dt, device=q.device) for t in (q, k, v))
-    for what, t, like in zip(("grad_q", "grad_k", "grad_v"), out, (q, k, v)):
-        _check_tensor(name, what, t, tuple(like.shape), dt, q.device)
-        _set_rows(op, what, t)
-    _set_rows(op, "ctx", ctx)
-    _set_rows(op, "grad_ctx", grad_ctx)
-    op.d_lse = lse.data_ptr()
-
-    def call(work, work_bytes, stream):
-        op.d_work, op.work_bytes = work, work_bytes
-        return lib().mt_op_packed_attention_grad(C.byref(op), stream)
-    _run(name, q.device, lib().mt_op_packed_attention_work(C.byref(op), 1), call)
+        out = [torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
+    _attention_call("mt_op_packed_attention_grad", "mt_op_packed_attention_grad", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse,
+                    (grad_ctx, *out))
     return tuple(out)
 
 
 def _vocab_loss(name, precision, x, W, labels):
     import torch
-    dt = _act_type(name, precision)
-    _check_tensor(name, "x", x, (None, None), dt, x.device)
-    _check_tensor(name, "W", W, (None, x.shape[1]), dt, x.device)
-    _check_tensor(name, "labels", labels, (x.shape[0],), torch.int32, x.device)
-    return x.shape[0], x.shape[1], W.shape[0]
+    dt, gpu = _act_type(name, precision), x.get_device()
+    (n, h), (v, _) = _dims(name, "x", x, 2), _dims(name, "W", W, 2)
+    _check(name, "x", x, (n, h), dt, gpu)
+    _check(name, "W", W, (v, h), dt, gpu)
+    _check(name, "labels", labels, (n,), torch.int32, gpu)
+    return n, h, v, gpu
 
 
 def op_vocab_loss(precision, x, W, labels):
     """mt_op_vocab_loss: x [tokens][hidden], W [vocab][hidden], labels int32 [tokens] (outside the vocabulary: none); returns the losses and the
     statistics for the gradient, float32 [tokens] each."""
     import torch
-    n, h, v = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
-    loss, lse = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
-    _run("mt_op_vocab_loss", x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
+    n, h, v, gpu = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
+    loss, lse = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
+    _run("mt_op_vocab_loss", gpu, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
         precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), n, h, v, work, size, stream))
     return loss, lse
 
@@ -720,14 +716,14 @@ def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
     op_vocab_loss's lse."""
     import torch
     name = "mt_op_vocab_loss_grad"
-    n, h, v = _vocab_loss(name, precision, x, W, labels)
-    _check_tensor(name, "lse", lse, (n,), torch.float32, x.device)
-    _check_tensor(name, "weight", weight, (n,), torch.float32, x.device)
+    n, h, v, gpu = _vocab_loss(name, precision, x, W, labels)
+    _check(name, "lse", lse, (n,), torch.float32, gpu)
+    _check(name, "weight", weight, (n,), torch.float32, gpu)
     dx = torch.empty((n, h), dtype=x.dtype, device=x.device)
     dw = torch.empty((v, h), dtype=torch.float32 if out_f32 else x.dtype, device=x.device)
-    _run(name, x.device, lib().mt_op_vocab_loss_work(precision, n, h, v, 1), lambda work, size, stream: lib().mt_op_vocab_loss_grad(
-        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), lse.data_ptr(), weight.data_ptr(), dx.data_ptr(), dw.data_ptr(), 1 if out_f32 else 0, n, h, v, work,
-        size, stream))
+    _run(name, gpu, lib().mt_op_vocab_loss_work(precision, n, h, v, 1), lambda work, size, stream: lib().mt_op_vocab_loss_grad(
+        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), lse.data_ptr(), weight.data_ptr(), dx.data_ptr(), dw.data_ptr(),
+        1 if out_f32 else 0, n, h, v, work, size, stream))
     return dx, dw
 
 
@@ -735,14 +731,15 @@ def op_embedding(precision, table, ids, scale=1.0, out=None):
     """mt_op_embedding: scale * table[ids] for int32 ids [n]; rows of zeros for ids outside the table."""
     import torch
     name = "mt_op_embedding"
-    dt = _act_type(name, precision)
-    _check_tensor(name, "table", table, (None, None), dt, table.device)
-    _check_tensor(name, "ids", ids, (None,), torch.int32, table.device)
-    n, (v, h) = ids.shape[0], table.shape
+    dt, gpu = _act_type(name, precision), table.get_device()
+    (n,), (v, h) = _dims(name, "ids", ids, 1), _dims(name, "table", table, 2)
+    _check(name, "table", table, (v, h), dt, gpu)
+    _check(name, "ids", ids, (n,), torch.int32, gpu)
     if out is None:
         out = torch.empty((n, h), dtype=dt, device=table.device)
-    _check_tensor(name, "out", out, (n, h), dt, table.device)
-    _run(name, table.device, 0, lambda work, size, stream: lib().mt_op_embedding(
+    else:
+        _check(name, "out", out, (n, h), dt, gpu)
+    _run(name, gpu, 0, lambda work, size, stream: lib().mt_op_embedding(
         precision, table.data_ptr(), table.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), n, v, h, stream))
     return out
 
@@ -752,17 +749,17 @@ def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add
     to instead."""
     import torch
     name = "mt_op_embedding_grad"
-    dt = _act_type(name, precision)
-    _check_tensor(name, "ids", ids, (None,), torch.int32, grad.device)
-    n, h = ids.shape[0], grad.shape[-1]
-    _check_tensor(name, "grad", grad, (n, h), dt, grad.device)
-    out = add_to
-    if out is None:
+    dt, gpu = _act_type(name, precision), grad.get_device()
+    (n, h), (m,) = _dims(name, "grad", grad, 2), _dims(name, "ids", ids, 1)
+    _check(name, "grad", grad, (m, h), dt, gpu)
+    _check(name, "ids", ids, (m,), torch.int32, gpu)
+    if add_to is None:
         out = torch.empty((vocab, h), dtype=torch.float32 if out_f32 else dt, device=grad.device)
     else:
-        _check_tensor(name, "add_to", out, (vocab, h), torch.float32, grad.device)
-    _run(name, grad.device, lib().mt_op_embedding_grad_work(precision, n, vocab, h), lambda work, size, stream: lib().mt_op_embedding_grad(
-        precision, grad.data_ptr(), grad.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), 1 if out.dtype == torch.float32 else 0,
+        out = add_to
+        _check(name, "add_to", out, (vocab, h), torch.float32, gpu)
+    _run(name, gpu, lib().mt_op_embedding_grad_work(precision, n, vocab, h), lambda work, size, stream: lib().mt_op_embedding_grad(
+        precision, grad.data_ptr(), grad.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), 1 if out.dtype is torch.float32 else 0,
         0 if add_to is None else 1, n, vocab, h, work, size, stream))
     return out
 
