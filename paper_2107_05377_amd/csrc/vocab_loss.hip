@@ -18,30 +18,38 @@ namespace mt {
 namespace {
 
 
-// ---- the labelled tokens, in order: index[0 .. *count)
+// ---- the labelled tokens, in order: index[0 .. *count).  One workgroup, 8 tokens a thread at a time (8192 tokens: one round).
 __global__ __launch_bounds__(1024) void label_index_kernel(const int32_t* labels, int tokens, int vocab, int32_t* count, int32_t* index)
 {
-    __shared__ int wave_n[16];
-    __shared__ int base;
+    __shared__ int wave_n[2][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (threadIdx.x == 0) base = 0;
-    for (int t0 = 0; t0 < tokens; t0 += 1024) {
-        const int t = t0 + threadIdx.x;
-        const bool has = t < tokens && (uint32_t)labels[t] < (uint32_t)vocab;
-        const uint64_t b = __ballot(has);
-        if (lane == 0) wave_n[wave] = __popcll(b);
+    int base = 0, turn = 0;
+    for (int t0 = 0; t0 < tokens; t0 += 8192, turn ^= 1) {
+        // a wavefront's 512 tokens as 8 rows of 64
+        const int first = t0 + wave * 512 + lane;
+        uint64_t has[8];
+        int l[8], mine = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) l[k] = first + k * 64 < tokens ? labels[first + k * 64] : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            has[k] = __ballot((uint32_t)l[k] < (uint32_t)vocab);
+            mine += __popcll(has[k]);
+        }
+        if (lane == 0) wave_n[turn][wave] = mine;
         __syncthreads();
-        int before = base, all = 0;
+        int at = base;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            before += i < wave ? wave_n[i] : 0;
-            all += wave_n[i];
+            at += i < wave ? wave_n[turn][i] : 0;
+            base += wave_n[turn][i];
         }
-        if (has) index[before + __popcll(b & ((1ull << lane) - 1))] = t;
-        __syncthreads();
-        if (threadIdx.x == 0) base += all;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if ((has[k] >> lane) & 1) index[at + __popcll(has[k] & ((1ull << lane) - 1))] = first + k * 64;
+            at += __popcll(has[k]);
+        }
     }
-    __syncthreads();
     if (threadIdx.x == 0) *count = base;
 }
 
@@ -340,16 +348,15 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabLoss p, const int3
 }
 
 // ---- gradient
-// the labelled rows of x behind one another
+// the labelled rows of x behind one another: a workgroup a row
 template <typename E>
 __global__ __launch_bounds__(256) void labelled_rows_kernel(VocabLoss p, const int32_t* count, const int32_t* index, typename E::elem* out)
 {
-    const int per = p.hidden / E::EPC, n = *count;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(at / per), c = (int)(at - (int64_t)row * per) * E::EPC;
-    if (row >= n) return;
-    *reinterpret_cast<typename E::frag*>(out + (int64_t)row * p.hidden + c) =
-        *reinterpret_cast<const typename E::frag*>(static_cast<const typename E::elem*>(p.x) + index[row] * p.ldx + c);
+    const int row = blockIdx.x;
+    if (row >= *count) return;
+    const typename E::elem* from = static_cast<const typename E::elem*>(p.x) + index[row] * p.ldx;
+    for (int c = threadIdx.x * E::EPC; c < p.hidden; c += blockDim.x * E::EPC)
+        *reinterpret_cast<typename E::frag*>(out + (int64_t)row * p.hidden + c) = *reinterpret_cast<const typename E::frag*>(from + c);
 }
 
 // dz of one piece of the vocabulary [piece0, piece0 + width) (columns beyond the vocabulary: 0), rows beyond the labelled ones up to a whole slice: 0
@@ -475,29 +482,37 @@ __global__ __launch_bounds__((Pick<E, true, true, C>::P::NT)) void vocab_dw_kern
     }
 }
 
-// dx: the ranges' sums put together and rounded, in the tokens' places; zeros for tokens without a label
+// dx: the ranges' sums put together and rounded, in the tokens' places; zeros for tokens without a label.  A workgroup a row.
 template <typename E>
 __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const int32_t* count, const int32_t* index, const float* part, Ranges ranges, int bm, int bn)
 {
-    const int per = p.hidden / 4, n = *count;
     typedef typename E::elem out4 __attribute__((ext_vector_type(4)));
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(at / per), c = (int)(at - (int64_t)row * per) * 4;
-    if (row >= p.tokens) return;
+    const int row = blockIdx.x, n = *count;
     auto* dx = static_cast<typename E::elem*>(p.dx);
-    out4 o;
-    if ((uint32_t)p.labels[row] >= (uint32_t)p.vocab) {
+    if ((uint32_t)p.labels[row] >= (uint32_t)p.vocab)
+        for (int c = threadIdx.x * 4; c < p.hidden; c += blockDim.x * 4) {
+            out4 o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)0.f;
-        *reinterpret_cast<out4*>(dx + (int64_t)row * p.hidden + c) = o;
-    }
+            for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)0.f;
+            *reinterpret_cast<out4*>(dx + (int64_t)row * p.hidden + c) = o;
+        }
     if (row >= n) return;
-    const int splits = ranges.of((int64_t)((n + bn - 1) / bn) * ((p.hidden + bm - 1) / bm));
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(part + ((int64_t)s * n + row) * p.hidden + c);
+    const int splits = ranges.of((int64_t)((n + bn - 1) / bn) * ((p.hidden + bm - 1) / bm)), to = index[row];
+    for (int c = threadIdx.x * 4; c < p.hidden; c += blockDim.x * 4) {
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        for (int s0 = 0; s0 < splits; s0 += 8) {
+            f32x4 x[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)v[e];
-    *reinterpret_cast<out4*>(dx + (int64_t)index[row] * p.hidden + c) = o;
+            for (int s = 0; s < 8; ++s) x[s] = *reinterpret_cast<const f32x4*>(part + ((int64_t)min(s0 + s, splits - 1) * n + row) * p.hidden + c);
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s0 + s < splits) v += x[s];
+        }
+        out4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (typename E::elem)v[e];
+        *reinterpret_cast<out4*>(dx + (int64_t)to * p.hidden + c) = o;
+    }
 }
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -531,8 +546,8 @@ Plan grad_plan(int tokens, int hidden, int vocab)
 {
     const size_t es = E::SIZE, rows = (size_t)(tokens + 63) / 64 * 64;
     Plan p;
-    // pieces of the vocabulary: dz of at most 256 MB, the size of the last-level cache
-    const size_t fit = (size_t)(256u << 20) / (rows * es) / 256 * 256, whole = ((size_t)vocab + 255) / 256 * 256;
+    // pieces of the vocabulary: dz of at most 512 MB
+    const size_t fit = (size_t)(512u << 20) / (rows * es) / 256 * 256, whole = ((size_t)vocab + 255) / 256 * 256;
     p.piece = (int)std::min(whole, std::max<size_t>(fit, 1024));
     const int kind = blocks_for<E>(tokens, vocab), bm = kind == BIG ? 256 : 128, bn = kind == BIG ? 256 : kind == MID ? 128 : 32, h_blocks = (hidden + bm - 1) / bm;
     p.ranges = Ranges{std::max(1, std::min(64, p.piece / 256)), kind == BIG ? 256 : 512};
@@ -592,7 +607,7 @@ hipError_t gradient_of(const VocabLoss& p, hipStream_t stream)
     float* part = reinterpret_cast<float*>(ws + pl.part);
     label_index_kernel<<<1, 1024, 0, stream>>>(p.labels, p.tokens, p.vocab, count, index);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    labelled_rows_kernel<E><<<(unsigned)(((int64_t)p.tokens * (p.hidden / E::EPC) + 255) / 256), 256, 0, stream>>>(p, count, index, xc);
+    labelled_rows_kernel<E><<<p.tokens, std::min(256, (p.hidden / E::EPC + 63) / 64 * 64), 0, stream>>>(p, count, index, xc);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return with_blocks<E>(blocks_for<E>(p.tokens, p.vocab), [&](auto c) {
         constexpr int C = c.value, CW = C == FEW ? MID : C;      // (dW has no tokens among its blocks)
@@ -620,7 +635,7 @@ hipError_t gradient_of(const VocabLoss& p, hipStream_t stream)
             else vocab_dw_kernel<E, elem, CW><<<(unsigned)grid_w, PW::NT, PW::LDS, stream>>>(p, count, dz, xc, v0, width);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        vocab_dx_rows_kernel<E><<<(unsigned)(((int64_t)p.tokens * (p.hidden / 4) + 255) / 256), 256, 0, stream>>>(p, count, index, part, pl.ranges, PX::BM, PX::BN);
+        vocab_dx_rows_kernel<E><<<p.tokens, std::min(256, (p.hidden / 4 + 63) / 64 * 64), 0, stream>>>(p, count, index, part, pl.ranges, PX::BM, PX::BN);
         return hipGetLastError();
     });
 }
