@@ -357,7 +357,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 && UB == 1 
     constexpr int BM = F::BM, TK = F::TK, NW = F::NW, BYTES = F::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];      // the ring of keys and values
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
+    const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, false>(p, item, group, BM, keys_each, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys
 {
     typedef typename E::elem elem;
     constexpr int ROW = DP + 4, COLS = DP / 64;
-    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
+    const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<4, false, true>(p, item, group, BM, keys_each, s) || s.chunks == 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -569,7 +569,7 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* 
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3, all = (int64_t)p.total_q * p.heads;
     const int part = threadIdx.x & 7;
     if (at >= all) return;
-    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads), group = p.heads / p.kv_heads, kvh = head / group;
+    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads), group = p.group, kvh = head / group;
     const elem* o = static_cast<const elem*>(p.ctx) + row * p.o_row + head * p.o_head;
     const elem* g = static_cast<const elem*>(p.dctx) + row * p.g_row + head * p.g_head;
     float sum = 0.f;
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
     constexpr int BM = R::BM, TK = R::TK, NW = R::NW, BYTES = R::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
+    const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, false>(p, item, group, BM, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
@@ -697,10 +697,10 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
 template <typename E, int DP, int KW, int RW, int STAGES>
 struct KeyGrad {
     using T = Tile<E, DP>;
-    // a stage: rows of q, rows of dctx, 256 bytes of every wavefront's: lse, delta and copies of them
+    // a stage: rows of q, rows of dctx, 256 bytes of every wavefront's: lse and delta of 64 rows, of the next 64 ..
     static constexpr int NW = KW * RW, BN = KW * 32, TQ = RW * 32, BYTES = TQ * T::ROWB, STAGE = 2 * BYTES + NW * 256, LPS = 2 * BYTES / 1024 / NW + 1;
     static constexpr int LDS = std::max(STAGES * STAGE, KW * (RW - 1) * DP * 64 * 4);
-    static_assert(LDS <= 160 * 1024 && TQ <= 64 && NW >= 2, "");
+    static_assert(LDS <= 160 * 1024 && TQ <= NW * 32, "");
 };
 
 template <typename E, int DP, int KW, int RW, int STAGES>
@@ -712,7 +712,7 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
     constexpr int BN = G::BN, TQ = G::TQ, NW = G::NW, BYTES = G::BYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = lds_address(lds);
-    const int group = p.heads / p.kv_heads, item = blockIdx.x / p.kv_heads, kvh = blockIdx.x - item * p.kv_heads;
+    const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, true>(p, item, 1, BN, 0, s)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
@@ -748,7 +748,7 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
         const uint32_t to = lds0 + stage_at * G::STAGE;
         rows_q.fetch(rt, rows - 1, to);
         rows_g.fetch(rt, rows - 1, to + BYTES);
-        load_to_lds_4(my_stat + min(rt * TQ + lane, rows - 1), to + 2 * BYTES + wave * 256);
+        load_to_lds_4(my_stat + min(rt * TQ + (wave >> 1) * 64 + lane, rows - 1), to + 2 * BYTES + wave * 256);
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
         if (rt + STAGES - 1 < n_tiles) fetch(rt + STAGES - 1, at == 0 ? STAGES - 1 : at - 1);
         const unsigned char* tq = lds + at * G::STAGE;
         const unsigned char* tg = tq + BYTES;
-        const float* in_lse = reinterpret_cast<const float*>(tg + BYTES) + rw * 32;
+        const float* in_lse = reinterpret_cast<const float*>(tg + BYTES) + (rw >> 1) * 128 + (rw & 1) * 32;
         const float* in_delta = in_lse + 64;
         const int b0 = rt * TQ + rw * 32;
         if (b0 < rows && b0 + 31 >= row_first) {
@@ -889,13 +889,13 @@ hipError_t forward_of(const PackedAttn& p, hipStream_t stream)
 template <typename E, int DP>
 hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
 {
-    constexpr int ROWB = Tile<E, DP>::ROWB, SQ = ROWB == 128 ? 3 : 2, SK = ROWB == 512 ? 2 : 3;
-    using G = KeyGrad<E, DP, 2, 2, SK>;
+    constexpr int ROWB = Tile<E, DP>::ROWB, SQ = ROWB == 128 ? 3 : 2, SK = ROWB == 512 || ROWB == 128 ? 2 : 3, A = ROWB == 128 ? 1 : 2, B = ROWB == 128 ? 4 : 2;
+    using G = KeyGrad<E, DP, A, B, SK>;
     using R = RowGrad<E, DP, 2, 2, SQ>;
     static std::atomic<uint64_t> done_q{0}, done_k{0};
     hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dq_kernel<E, DP, 2, 2, SQ>), R::LDS, done_q);
     if (e != hipSuccess) return e;
-    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, 2, 2, SK>), G::LDS, done_k);
+    e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, A, B, SK>), G::LDS, done_k);
     if (e != hipSuccess) return e;
     float* stat = static_cast<float*>(p.work);
     const int64_t n = (int64_t)p.total_q * p.heads;
@@ -903,7 +903,7 @@ hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
     if (tiles_q * p.kv_heads > 0x7FFFFFFF || tiles_k * p.kv_heads > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
     packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    packed_dkv_kernel<E, DP, 2, 2, SK><<<(unsigned)(tiles_k * p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
+    packed_dkv_kernel<E, DP, A, B, SK><<<(unsigned)(tiles_k * p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     packed_dq_kernel<E, DP, 2, 2, SQ><<<(unsigned)(tiles_q * p.kv_heads), R::NW * 64, R::LDS, stream>>>(p, stat);
     return hipGetLastError();

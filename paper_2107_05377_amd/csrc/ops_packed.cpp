@@ -54,6 +54,7 @@ PackedAttn attention_args(const mt_packed_attention* op)
     p.n_seqs = op->n_seqs;
     p.heads = op->heads;
     p.kv_heads = op->kv_heads;
+    p.group = op->heads / op->kv_heads;
     p.d = op->width;
     p.total_q = op->total_q;
     p.total_k = op->total_k;

@@ -17,7 +17,7 @@ struct PackedAttn {
     const int32_t *q_start, *k_start;   // [n_seqs + 1]
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, g_row, g_head;      // o: ctx / out, g: dctx
     int64_t dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
-    int32_t n_seqs, heads, kv_heads, d, total_q, total_k, causal;
+    int32_t n_seqs, heads, kv_heads, group, d, total_q, total_k, causal;     // group: heads / kv_heads
     float scale;
     void* work;
     size_t work_bytes;
