@@ -136,6 +136,13 @@ __device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v,
 
 // Workgroups: key heads first, so that the tiles of a sequence, whose cost falls from the first to the last, end a launch with the cheapest, and a key head's
 // workgroups share an XCD where there are 8 key heads or a part of 8.
+// What is found is the same in all lanes; the compiler is told, so that what is reckoned from it is scalar work.
+__device__ __forceinline__ Seq same_in_all(const Seq& s)
+{
+    const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return Seq{u(s.q0), u(s.lq), u(s.k0), u(s.lk), u(s.tile), u(s.chunk), u(s.chunks), u(s.first)};
+}
+
 // Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with
 // keys_each > 0 its sequence's chunks of that many keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are
 // brought inside, a sequence that would end before it starts is empty.  A workgroup looks through 64 sequences for each of its wavefronts at a time:
@@ -207,18 +214,13 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
                 s.chunks = found[2];
                 first_items = found[3];
             }
-            // (the same in all lanes, which the compiler is told: what is reckoned from them is scalar work)
-            seq = __builtin_amdgcn_readfirstlane(seq);
-            mine = __builtin_amdgcn_readfirstlane(mine);
-            s.chunks = __builtin_amdgcn_readfirstlane(s.chunks);
             s.tile = BY_TILE ? mine : mine / s.chunks;
             s.chunk = BY_TILE ? 0 : mine - s.tile * s.chunks;
-            s.first = BY_TILE ? __builtin_amdgcn_readfirstlane(first_items) + s.tile * s.chunks : w - s.chunk;
-            const auto at = [](const int32_t* start, int i, int total) { return __builtin_amdgcn_readfirstlane(clamp_start(start[i], total)); };
-            s.q0 = at(p.q_start, seq, p.total_q);
-            s.lq = max(at(p.q_start, seq + 1, p.total_q) - s.q0, 0);
-            s.k0 = at(p.k_start, seq, p.total_k);
-            s.lk = max(at(p.k_start, seq + 1, p.total_k) - s.k0, 0);
+            s.first = BY_TILE ? first_items + s.tile * s.chunks : w - s.chunk;
+            s.q0 = clamp_start(p.q_start[seq], p.total_q);
+            s.lq = max(clamp_start(p.q_start[seq + 1], p.total_q) - s.q0, 0);
+            s.k0 = clamp_start(p.k_start[seq], p.total_k);
+            s.lk = max(clamp_start(p.k_start[seq + 1], p.total_k) - s.k0, 0);
             return true;
         }
         base += all;
@@ -360,16 +362,18 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 && UB == 1 
     const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, false>(p, item, group, BM, keys_each, s)) return;
+    s = same_in_all(s);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
     const int r0 = (tiles - 1 - s.tile) * BM;                                 // the rows that see most first
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;                    // query i sees keys up to i + shift
     const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
+    const auto limit_all = [&](int r) { return __builtin_amdgcn_readfirstlane(limit_of(r)); };         // of a row that is the same in all lanes
     const int my_row = min(r0 + rw * 32 + l32, rows - 1);
     const int tok = my_row / group, head = kvh * group + my_row - tok * group;
-    const int limit = limit_of(my_row), wave_min = limit_of(r0 + rw * 32), wave_max = limit_of(r0 + rw * 32 + 31);
-    int n_keys = limit_of(r0 + BM - 1) + 1, t0 = 0;
+    const int limit = limit_of(my_row), wave_min = limit_all(r0 + rw * 32), wave_max = limit_all(r0 + rw * 32 + 31);
+    int n_keys = limit_all(r0 + BM - 1) + 1, t0 = 0;
     if (keys_each > 0) {
         t0 = s.chunk * (keys_each / TK);
         n_keys = min(n_keys, (s.chunk + 1) * keys_each);
@@ -606,16 +610,18 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
     const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, false>(p, item, group, BM, 0, s)) return;
+    s = same_in_all(s);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM;
     const int r0 = (tiles - 1 - s.tile) * BM;
     const int shift = p.causal ? s.lk - s.lq : 0x40000000;
     const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
+    const auto limit_all = [&](int r) { return __builtin_amdgcn_readfirstlane(limit_of(r)); };         // of a row that is the same in all lanes
     const int my_row = min(r0 + rw * 32 + l32, rows - 1);
     const int tok = my_row / group, head = kvh * group + my_row - tok * group;
-    const int limit = limit_of(my_row), wave_min = limit_of(r0 + rw * 32), wave_max = limit_of(r0 + rw * 32 + 31);
-    const int n_keys = limit_of(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
+    const int limit = limit_of(my_row), wave_min = limit_all(r0 + rw * 32), wave_max = limit_all(r0 + rw * 32 + 31);
+    const int n_keys = limit_all(r0 + BM - 1) + 1, n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
 
     const elem* K = static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head;
     const elem* V = static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head;
@@ -715,6 +721,7 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
     const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<NW, true>(p, item, 1, BN, 0, s)) return;
+    s = same_in_all(s);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
     const int kw = wave / RW, rw = wave % RW;
     const int rows = s.lq * group, n0 = s.tile * BN;
