@@ -150,18 +150,16 @@ __device__ __forceinline__ Seq same_in_all(const Seq& s)
 template <int NW, bool KEYS, bool BY_TILE = false>
 __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, int tile, int keys_each, Seq& s)
 {
-    __shared__ int wave_sum[NW][2], found[5];
+    __shared__ int wave_sum[NW][2], found[8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t* start = KEYS ? p.k_start : p.q_start;
-    const int total = KEYS ? p.total_k : p.total_q;
     int base = 0, base_items = 0;
     for (int b0 = 0; b0 < p.n_seqs; b0 += 64 * NW) {
         const bool one = p.n_seqs - b0 <= 64;               // every wavefront looks at the same sequences: nothing to exchange
         const int mine_b = b0 + (one ? lane : (int)threadIdx.x), b = min(mine_b, p.n_seqs - 1);
-        const int a = clamp_start(start[b], total), e = clamp_start(start[b + 1], total);
-        const int tiles = mine_b < p.n_seqs ? (int)(((int64_t)max(e - a, 0) * per + tile - 1) / tile) : 0;
-        int chunks = 1;
-        if (keys_each > 0) chunks = max(1, (max(clamp_start(p.k_start[b + 1], p.total_k) - clamp_start(p.k_start[b], p.total_k), 0) + keys_each - 1) / keys_each);
+        const int q0 = clamp_start(p.q_start[b], p.total_q), lq = max(clamp_start(p.q_start[b + 1], p.total_q) - q0, 0);
+        const int k0 = clamp_start(p.k_start[b], p.total_k), lk = max(clamp_start(p.k_start[b + 1], p.total_k) - k0, 0);
+        const int tiles = mine_b < p.n_seqs ? (int)(((int64_t)(KEYS ? lk : lq) * per + tile - 1) / tile) : 0;
+        const int chunks = keys_each > 0 ? max(1, (lk + keys_each - 1) / keys_each) : 1;
         const int n = BY_TILE ? tiles : tiles * chunks;
         int sum = n, items = tiles * chunks;
 #pragma unroll
@@ -192,35 +190,34 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
             items += before_items;
         }
         if (w < base + all) {
-            int seq, mine, first_items, tiles_n;
+            int mine, first_items;
             if (one) {
-                const uint64_t past = __ballot(base + sum > w);
-                const int l = __ffsll((unsigned long long)past) - 1;
-                seq = b0 + l;
+                const int l = __ffsll((unsigned long long)__ballot(base + sum > w)) - 1;
                 mine = w - (base + __shfl(sum, l) - __shfl(n, l));
                 s.chunks = __shfl(chunks, l);
-                tiles_n = __shfl(tiles, l);
-                first_items = base_items + __shfl(items, l) - tiles_n * s.chunks;
+                first_items = base_items + __shfl(items, l) - __shfl(tiles, l) * s.chunks;
+                s.q0 = __shfl(q0, l);
+                s.lq = __shfl(lq, l);
+                s.k0 = __shfl(k0, l);
+                s.lk = __shfl(lk, l);
             } else {
                 if (w >= base + sum - n && w < base + sum) {
-                    found[0] = mine_b;
-                    found[1] = w - (base + sum - n);
-                    found[2] = chunks;
-                    found[3] = base_items + items - tiles * chunks;
+                    const int put[7] = {w - (base + sum - n), chunks, base_items + items - tiles * chunks, q0, lq, k0, lk};
+#pragma unroll
+                    for (int i = 0; i < 7; ++i) found[i] = put[i];
                 }
                 __syncthreads();
-                seq = found[0];
-                mine = found[1];
-                s.chunks = found[2];
-                first_items = found[3];
+                mine = found[0];
+                s.chunks = found[1];
+                first_items = found[2];
+                s.q0 = found[3];
+                s.lq = found[4];
+                s.k0 = found[5];
+                s.lk = found[6];
             }
             s.tile = BY_TILE ? mine : mine / s.chunks;
             s.chunk = BY_TILE ? 0 : mine - s.tile * s.chunks;
             s.first = BY_TILE ? first_items + s.tile * s.chunks : w - s.chunk;
-            s.q0 = clamp_start(p.q_start[seq], p.total_q);
-            s.lq = max(clamp_start(p.q_start[seq + 1], p.total_q) - s.q0, 0);
-            s.k0 = clamp_start(p.k_start[seq], p.total_k);
-            s.lk = max(clamp_start(p.k_start[seq + 1], p.total_k) - s.k0, 0);
             return true;
         }
         base += all;
@@ -855,7 +852,7 @@ Deal deal_of(int n_seqs, int total_q, int total_k, int heads, int kv_heads)
     d.items = d.tiles;
     if (d.rows_each == 32 && d.tiles * kv_heads < 1024) {
         // few workgroups: keys dealt out so that there are about 1024, 256 keys each at least (what a workgroup needs to get going costs as much)
-        const int64_t each = std::max<int64_t>(256, ((int64_t)total_k * kv_heads / 1024 + 255) / 256 * 256);
+        const int64_t each = std::max<int64_t>(512, ((int64_t)total_k * kv_heads / 1024 + 255) / 256 * 256);
         if (total_k > each) {
             d.keys_each = (int)each;
             // sum over sequences of (rows / 32 + 1) (keys / each + 1)
