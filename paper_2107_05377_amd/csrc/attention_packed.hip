@@ -160,6 +160,29 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
         const int k0 = clamp_start(p.k_start[b], p.total_k), lk = max(clamp_start(p.k_start[b + 1], p.total_k) - k0, 0);
         const int tiles = mine_b < p.n_seqs ? (int)(((int64_t)(KEYS ? lk : lq) * per + tile - 1) / tile) : 0;
         const int chunks = keys_each > 0 ? max(1, (lk + keys_each - 1) / keys_each) : 1;
+        if (!BY_TILE && keys_each == 0 && p.n_seqs > 1 && p.n_seqs <= 64) {
+            // few sequences: the tiles that are followed by most others of their sequence first, in all sequences (the longest sequence last in the
+            // list would otherwise end the launch with its longest tiles).  behind(d): tiles followed by d others or more.
+            const auto behind = [&](int d) { return wave_sum_int(max(tiles - d, 0)); };
+            if (w >= behind(0)) return false;
+            int lo = 1, hi = (int)wave_max((float)tiles);           // (less than 2^24 tiles: rows are numbered with 29 bits, 32 a tile)
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (behind(mid) <= w) hi = mid;
+                else lo = mid + 1;
+            }
+            const int nth = w - behind(lo);
+            const uint64_t have = __ballot(tiles >= lo);
+            const int l = __ffsll((unsigned long long)__ballot(tiles >= lo && __popcll(have & ((1ull << lane) - 1)) == nth)) - 1;
+            s.chunk = s.first = 0;
+            s.chunks = 1;
+            s.tile = __shfl(tiles, l) - lo;
+            s.q0 = __shfl(q0, l);
+            s.lq = __shfl(lq, l);
+            s.k0 = __shfl(k0, l);
+            s.lk = __shfl(lk, l);
+            return true;
+        }
         const int n = BY_TILE ? tiles : tiles * chunks;
         int sum = n, items = tiles * chunks;
 #pragma unroll
