@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys
     if (p.lse && lane == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
 }
 
-// What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and delta = dctx . ctx.  8 lanes a row.
+// What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and -delta = -dctx . ctx.  8 lanes a row.
 template <typename E>
 __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* stat)
 {
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* 
     sum += __shfl_xor(sum, 4);
     const int64_t to = (int64_t)kvh * p.total_q * group + (int64_t)row * group + head - kvh * group;
     if (part == 0) stat[to] = p.lse_in[(int64_t)head * p.total_q + row] * kLog2e;
-    if (part == 1) stat[all + to] = sum;
+    if (part == 1) stat[all + to] = -sum;
 }
 
 // dq: rows fixed, keys pass by.  RW blocks of 32 rows, each with KW wavefronts that take a block of 32 keys of a tile each.
@@ -661,7 +661,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
     load_row<E, DP>(gf, static_cast<const elem*>(p.dctx) + (int64_t)(s.q0 + tok) * p.g_row + head * p.g_head, p.d, half);
     const float c = p.scale * kLog2e;
     const float* my_stat = stat + ((int64_t)kvh * p.total_q + s.q0) * group + my_row;
-    const float lse = my_stat[0], dl = my_stat[(int64_t)p.total_q * p.heads];
+    const float lse = my_stat[0], less = my_stat[(int64_t)p.total_q * p.heads];
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
         for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
     loaded(qf);
     loaded(gf);
-    asm volatile("" ::"v"(lse), "v"(dl));
+    asm volatile("" ::"v"(lse), "v"(less));
     int at = 0;
     for (int kt = 0; kt < n_tiles; ++kt, at = at + 1 == STAGES ? 0 : at + 1) {
         tile_landed<STAGES, R::LPS>(n_tiles - 1 - kt);
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 
         }
         const bool cut = key0 + 31 > wave_min;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] - dl);
+        for (int i = 0; i < 16; ++i) sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * (dp[i] + less);
         if (cut) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = key0 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? sc[i] : 0.f;
@@ -789,12 +789,20 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
         const unsigned char* tq = lds + at * G::STAGE;
         const unsigned char* tg = tq + BYTES;
         const float* in_lse = reinterpret_cast<const float*>(tg + BYTES) + (rw >> 1) * 128 + (rw & 1) * 32;
-        const float* in_delta = in_lse + 64;
+        const float* in_delta = in_lse + 64;      // (-delta)
         const int b0 = rt * TQ + rw * 32;
         if (b0 < rows && b0 + 31 >= row_first) {
+            // dctx v^T is added to -delta, whose rows are the accumulators' as they lie in LDS
             f32x16 sc, dp;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 less = *reinterpret_cast<const f32x4*>(in_delta + 8 * g + 4 * half);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sc[4 * g + j] = 0.f;
+                    dp[4 * g + j] = less[j];
+                }
+            }
 #pragma unroll
             for (int ks = 0; ks < DP / E::KS; ++ks) {
                 sc = E::mma(T::row_frag(tq, rw * 32 + l32, ks, half), kf[ks], sc);
@@ -804,12 +812,12 @@ __global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) v
             const auto sees = [&](int k) { return b0 + k >= my_first && b0 + k < rows; };
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(in_lse + 8 * g + 4 * half), dl = *reinterpret_cast<const f32x4*>(in_delta + 8 * g + 4 * half);
+                const f32x4 l = *reinterpret_cast<const f32x4*>(in_lse + 8 * g + 4 * half);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * g + j;
                     sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -l[j]));
-                    dp[i] = sc[i] * (dp[i] - dl[j]);
+                    dp[i] = sc[i] * dp[i];
                 }
             }
             if (cut) {
