@@ -671,10 +671,10 @@ def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, s
 def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, scale=None, out=None, want_lse=False):
     """mt_op_packed_attention: q [queries][heads][width], k, v [keys][kv_heads][width] (any strides of rows and heads), q_start, k_start int32
     [sequences + 1]; scale None: 1 / sqrt(width).  Returns the context [queries][heads][width] (`out`, or zeros where no sequence is) and with want_lse
-    the statistics [heads][queries] float32 for the gradient."""
+    the statistics [heads][queries] float32 for the gradient (unspecified where no sequence is)."""
     import torch
     ctx = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    lse = q.new_full((q.shape[1], q.shape[0]), float("-inf"), dtype=torch.float32) if want_lse else None
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if want_lse else None
     _attention_call("mt_op_packed_attention", "mt_op_packed_attention", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse)
     return (ctx, lse) if want_lse else ctx
 

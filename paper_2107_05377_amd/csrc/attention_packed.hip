@@ -3,7 +3,7 @@
 // Sequence b owns query rows q_start[b] .. q_start[b+1]-1 and key rows k_start[b] .. ; with Lq and Lk of them, query i sees the keys
 // j <= i + Lk - Lq (causal: the last query sees the last key) or all Lk.  Query head a reads key head a / group.
 //   S = scale q k^T,  lse = log sum_visible exp S,  P = exp(S - lse),  ctx = P v
-//   delta = dctx . ctx,  dS = P (dctx v^T - delta),  dv = P^T dctx,  dq = scale dS k,  dk = scale dS^T q
+//   delta = sum P (dctx v^T) = dctx . ctx,  dS = P (dctx v^T - delta),  dv = P^T dctx,  dq = scale dS k,  dk = scale dS^T q
 //
 // Rows.  The query heads of a group share keys and values, so their rows are one list: row r of a (sequence, key head) is query r / group
 // of head r % group.  A group of 4 heads then needs its keys once, a single token has `group` rows, and dk, dv come out summed over the group.
@@ -585,29 +585,83 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys
     if (p.lse && lane == 0) p.lse[(int64_t)head * p.total_q + s.q0 + tok] = limit < 0 ? -INFINITY : fmaf(ref, p.scale, __builtin_amdgcn_logf(sum) * kLn2);
 }
 
-// What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and -delta = -dctx . ctx.  8 lanes a row.
-template <typename E>
-__global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn p, float* stat)
+// What the gradient needs of a row, in the order of the packed rows (key head, query, head of the group): lse log2e and -delta.
+// delta = dctx . ctx = sum_j P_ij (dctx_i . v_j).  ctx has been rounded, which delta hardly notices where a row averages many values, but rows of few keys
+// have the largest gradients: in bfloat16, tiles whose rows see at most kFewKeys keys take the second form, from the weights themselves.  Against float64, dq
+// and dk of sequences of a few tens of tokens are off by 0.0024 (2-norm, relative) instead of 0.0032, of 300 to 4001 tokens 0.0024 instead of 0.0025; what
+// is left is the rounding of dS and of the results.
+constexpr int kFewKeys = 128;
+template <typename E, int DP>
+__global__ __launch_bounds__(256) void packed_stat_kernel(PackedAttn p, float* stat)
 {
+    using T = Tile<E, DP>;
     typedef typename E::elem elem;
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3, all = (int64_t)p.total_q * p.heads;
-    const int part = threadIdx.x & 7;
-    if (at >= all) return;
-    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads), group = p.group, kvh = head / group;
-    const elem* o = static_cast<const elem*>(p.ctx) + row * p.o_row + head * p.o_head;
-    const elem* g = static_cast<const elem*>(p.dctx) + row * p.g_row + head * p.g_head;
+    constexpr int NW = 4, BM = NW * 32, TK = 32, BYTES = TK * T::ROWB, LPS = 2 * BYTES / 1024 / NW;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * BYTES];
+    const uint32_t lds0 = lds_address(lds);
+    const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
+    Seq s;
+    if (!find_tile<NW, false>(p, item, group, BM, 0, s)) return;
+    s = same_in_all(s);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+    const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r0 = (tiles - 1 - s.tile) * BM;
+    const int shift = p.causal ? s.lk - s.lq : 0x40000000;
+    const auto limit_of = [&](int r) { return min(min(r, rows - 1) / group + shift, s.lk - 1); };
+    const auto limit_all = [&](int r) { return __builtin_amdgcn_readfirstlane(limit_of(r)); };
+    const int my_row = min(r0 + wave * 32 + l32, rows - 1);
+    const int tok = my_row / group, head = kvh * group + my_row - tok * group;
+    const int limit = limit_of(my_row), n_keys = limit_all(r0 + BM - 1) + 1;
+
+    typename E::frag gf[DP / E::KS], of[DP / E::KS];
+    load_row<E, DP>(gf, static_cast<const elem*>(p.dctx) + (int64_t)(s.q0 + tok) * p.g_row + head * p.g_head, p.d, half);
+    const float lse = p.lse_in[(int64_t)head * p.total_q + s.q0 + tok] * kLog2e;
     float sum = 0.f;
-    for (int c = part * E::EPC; c < p.d; c += 8 * E::EPC) {
-        const typename E::frag a = *reinterpret_cast<const typename E::frag*>(o + c), b = *reinterpret_cast<const typename E::frag*>(g + c);
+    if (E::SIZE == 4 || n_keys > kFewKeys) {
+        load_row<E, DP>(of, static_cast<const elem*>(p.ctx) + (int64_t)(s.q0 + tok) * p.o_row + head * p.o_head, p.d, half);
 #pragma unroll
-        for (int j = 0; j < E::EPC; ++j) sum = fmaf((float)a[j], (float)b[j], sum);
+        for (int ks = 0; ks < DP / E::KS; ++ks)
+#pragma unroll
+            for (int j = 0; j < E::EPC; ++j) sum = fmaf((float)gf[ks][j], (float)of[ks][j], sum);
+    } else {
+        load_row<E, DP>(of, static_cast<const elem*>(p.q) + (int64_t)(s.q0 + tok) * p.q_row + head * p.q_head, p.d, half);
+        loaded(gf);
+        loaded(of);
+        asm volatile("" ::"v"(lse));
+        const float c = p.scale * kLog2e;
+        Rows<E, DP, TK, NW> rows_k, rows_v;
+        rows_k.init(static_cast<const elem*>(p.k) + (int64_t)s.k0 * p.k_row + kvh * p.k_head, p.k_row, 0, 1, p.d);
+        rows_v.init(static_cast<const elem*>(p.v) + (int64_t)s.k0 * p.v_row + kvh * p.v_head, p.v_row, 0, 1, p.d);
+        const auto fetch = [&](int kt) {
+            rows_k.fetch(kt, s.lk - 1, lds0 + (kt & 1) * 2 * BYTES);
+            rows_v.fetch(kt, s.lk - 1, lds0 + (kt & 1) * 2 * BYTES + BYTES);
+        };
+        const int n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
+        if (n_tiles > 0) fetch(0);
+        for (int kt = 0; kt < n_tiles; ++kt) {
+            tile_landed<2, LPS>(0);
+            if (kt + 1 < n_tiles) fetch(kt + 1);
+            const unsigned char* tk = lds + (kt & 1) * 2 * BYTES;
+            const unsigned char* tv = tk + BYTES;
+            f32x16 sc, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < DP / E::KS; ++ks) {
+                sc = E::mma(T::row_frag(tk, l32, ks, half), of[ks], sc);
+                dp = E::mma(T::row_frag(tv, l32, ks, half), gf[ks], dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -lse)) * dp[i];
+                sum += kt * TK + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? w : 0.f;
+            }
+        }
     }
-    sum += __shfl_xor(sum, 1);
-    sum += __shfl_xor(sum, 2);
-    sum += __shfl_xor(sum, 4);
-    const int64_t to = (int64_t)kvh * p.total_q * group + (int64_t)row * group + head - kvh * group;
-    if (part == 0) stat[to] = p.lse_in[(int64_t)head * p.total_q + row] * kLog2e;
-    if (part == 1) stat[all + to] = -sum;
+    sum = lane_pair_sum<32>(sum);
+    if (half != 0 || r0 + wave * 32 + l32 >= rows) return;
+    float* to = stat + ((int64_t)kvh * p.total_q + s.q0) * group + my_row;
+    to[0] = lse;
+    to[(int64_t)p.total_q * p.heads] = -sum;
 }
 
 // dq: rows fixed, keys pass by.  RW blocks of 32 rows, each with KW wavefronts that take a block of 32 keys of a tile each.
@@ -933,10 +987,9 @@ hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
     e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_dkv_kernel<E, DP, A, B, SK>), G::LDS, done_k);
     if (e != hipSuccess) return e;
     float* stat = static_cast<float*>(p.work);
-    const int64_t n = (int64_t)p.total_q * p.heads;
-    const int64_t tiles_q = (int64_t)p.total_q * (p.heads / p.kv_heads) / R::BM + p.n_seqs, tiles_k = (int64_t)p.total_k / G::BN + p.n_seqs;
-    if (tiles_q * p.kv_heads > 0x7FFFFFFF || tiles_k * p.kv_heads > 0x7FFFFFFF || (n + 31) / 32 > 0x7FFFFFFF) return hipErrorInvalidValue;
-    packed_delta_kernel<E><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(p, stat);
+    const int64_t tiles_s = (int64_t)p.total_q * p.group / 128 + p.n_seqs, tiles_q = (int64_t)p.total_q * p.group / R::BM + p.n_seqs, tiles_k = (int64_t)p.total_k / G::BN + p.n_seqs;
+    if (tiles_q * p.kv_heads > 0x7FFFFFFF || tiles_k * p.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    packed_stat_kernel<E, DP><<<(unsigned)(tiles_s * p.kv_heads), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     packed_dkv_kernel<E, DP, A, B, SK><<<(unsigned)(tiles_k * p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
