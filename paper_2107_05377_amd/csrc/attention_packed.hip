@@ -360,6 +360,13 @@ __device__ __forceinline__ void store_cols(const f32x16 (&acc)[DP / 32], float b
         }
 }
 
+// wavefronts per SIMD that a kernel is compiled for: `narrow` for bfloat16 rows of up to 64 columns, 2 for wider ones and float32 ones of up to 64, 1 for the rest
+template <typename E, int DP>
+constexpr int waves_of(int narrow)
+{
+    return Tile<E, DP>::ROWB == 128 ? narrow : Tile<E, DP>::ROWB == 256 ? 2 : 1;
+}
+
 // RW x KW wavefronts: RW blocks of 32 rows, each with KW wavefronts that take UB blocks of 32 keys of a tile in turn and put their sums together at the
 // end.  p.work: with keys_each > 0 a tile's keys are dealt out to workgroups as well, whose sums a second launch puts together.
 template <typename E, int DP, int RW, int KW, int UB, int STAGES>
@@ -371,7 +378,7 @@ struct Forward {
 };
 
 template <typename E, int DP, int RW, int KW, int UB, int STAGES>
-__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 && UB == 1 ? 3 : 2) : 1)) void packed_forward_kernel(PackedAttn p, int keys_each)
+__global__ __launch_bounds__(RW * KW * 64, (waves_of<E, DP>(UB == 1 ? 3 : 2))) void packed_forward_kernel(PackedAttn p, int keys_each)
 {
     using F = Forward<E, DP, RW, KW, UB, STAGES>;
     using T = Tile<E, DP>;
@@ -673,7 +680,7 @@ struct RowGrad {
 };
 
 template <typename E, int DP, int RW, int KW, int STAGES>
-__global__ __launch_bounds__(RW * KW * 64, (E::SIZE == 2 ? (DP == 64 ? 3 : 2) : 1)) void packed_dq_kernel(PackedAttn p, const float* stat)
+__global__ __launch_bounds__(RW * KW * 64, (waves_of<E, DP>(3))) void packed_dq_kernel(PackedAttn p, const float* stat)
 {
     using R = RowGrad<E, DP, RW, KW, STAGES>;
     using T = Tile<E, DP>;
@@ -784,7 +791,7 @@ struct KeyGrad {
 };
 
 template <typename E, int DP, int KW, int RW, int STAGES>
-__global__ __launch_bounds__(KW * RW * 64, (E::SIZE == 2 && DP == 64 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
+__global__ __launch_bounds__(KW * RW * 64, (Tile<E, DP>::ROWB == 128 ? 2 : 1)) void packed_dkv_kernel(PackedAttn p, const float* stat)
 {
     using G = KeyGrad<E, DP, KW, RW, STAGES>;
     using T = Tile<E, DP>;
