@@ -590,13 +590,24 @@ def _refuse(name, text, code=MT_ERR_SHAPE):
     raise MTError(code, f"{name}: {text}")
 
 
+_torch = None
+
+
+def _t():
+    """torch, imported by the first call that needs it."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _act_type(name, precision):
-    import torch
     if precision == MT_BF16:
-        return torch.bfloat16
+        return _t().bfloat16
     if precision != MT_FP32_CHECK:
         _refuse(name, "MT_BF16 or MT_FP32_CHECK", MT_ERR_CONFIG)
-    return torch.float32
+    return _t().float32
 
 
 def _check(name, what, t, shape, dtype, gpu):
@@ -613,15 +624,16 @@ def _check(name, what, t, shape, dtype, gpu):
 
 
 def _dims(name, what, t, n):
-    if t.dim() != n:
-        _refuse(name, f"{what} has {t.dim()} dimensions, not {n}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != n:
+        _refuse(name, f"{what} has {len(shape)} dimensions, not {n}")
+    return shape
 
 
 def _run(name, gpu, work_bytes, call):
     """call(work pointer, work bytes, stream) with a workspace of its own, on GPU `gpu` and its current stream."""
-    import torch
-    if gpu != torch.cuda.current_device():
+    torch = _t()
+    if gpu != torch._C._cuda_getDevice():
         with torch.cuda.device(gpu):
             return _run(name, gpu, work_bytes, call)
     work = torch.empty(work_bytes, dtype=torch.uint8, device="cuda") if work_bytes else None
@@ -636,7 +648,7 @@ assert _ATTENTION.size == C.sizeof(mt_packed_attention)
 
 def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, scale, ctx, lse, grads=None):
     """The checks and the call of both attention entry points; grads: (grad_ctx, grad_q, grad_k, grad_v)."""
-    import torch
+    torch = _t()
     dt, gpu = _act_type(name, precision), q.get_device()
     (tq, heads, d), (tk, kv_heads, _) = _dims(name, "q", q, 3), _dims(name, "k", k, 3)
     n_starts = _dims(name, "q_start", q_start, 1)
@@ -672,7 +684,7 @@ def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, 
     """mt_op_packed_attention: q [queries][heads][width], k, v [keys][kv_heads][width] (any strides of rows and heads), q_start, k_start int32
     [sequences + 1]; scale None: 1 / sqrt(width).  Returns the context [queries][heads][width] (`out`, or zeros where no sequence is) and with want_lse
     the statistics [heads][queries] float32 for the gradient (unspecified where no sequence is)."""
-    import torch
+    torch = _t()
     ctx = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if want_lse else None
     _attention_call("mt_op_packed_attention", "mt_op_packed_attention", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse)
@@ -682,7 +694,7 @@ def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, 
 def op_packed_attention_grad(precision, grad_ctx, q, k, v, ctx, lse, q_start, k_start=None, causal=True, scale=None, out=None):
     """mt_op_packed_attention_grad: the gradients of q, k and v (`out`, three tensors, or new ones with zeros where no sequence is) from grad_ctx and the
     ctx and lse of op_packed_attention with the same arguments."""
-    import torch
+    torch = _t()
     if out is None:
         out = [torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
     _attention_call("mt_op_packed_attention_grad", "mt_op_packed_attention_grad", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse,
@@ -691,7 +703,7 @@ def op_packed_attention_grad(precision, grad_ctx, q, k, v, ctx, lse, q_start, k_
 
 
 def _vocab_loss(name, precision, x, W, labels):
-    import torch
+    torch = _t()
     dt, gpu = _act_type(name, precision), x.get_device()
     (n, h), (v, _) = _dims(name, "x", x, 2), _dims(name, "W", W, 2)
     _check(name, "x", x, (n, h), dt, gpu)
@@ -703,9 +715,9 @@ def _vocab_loss(name, precision, x, W, labels):
 def op_vocab_loss(precision, x, W, labels):
     """mt_op_vocab_loss: x [tokens][hidden], W [vocab][hidden], labels int32 [tokens] (outside the vocabulary: none); returns the losses and the
     statistics for the gradient, float32 [tokens] each."""
-    import torch
+    torch = _t()
     n, h, v, gpu = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
-    loss, lse = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
+    loss, lse = x.new_empty((2, n), dtype=torch.float32)
     _run("mt_op_vocab_loss", gpu, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
         precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), n, h, v, work, size, stream))
     return loss, lse
@@ -714,7 +726,7 @@ def op_vocab_loss(precision, x, W, labels):
 def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
     """mt_op_vocab_loss_grad: the gradients of x and of W (float32 with out_f32) for weight float32 [tokens], the gradient of each token's loss, and
     op_vocab_loss's lse."""
-    import torch
+    torch = _t()
     name = "mt_op_vocab_loss_grad"
     n, h, v, gpu = _vocab_loss(name, precision, x, W, labels)
     _check(name, "lse", lse, (n,), torch.float32, gpu)
@@ -729,14 +741,13 @@ def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
 
 def op_embedding(precision, table, ids, scale=1.0, out=None):
     """mt_op_embedding: scale * table[ids] for int32 ids [n]; rows of zeros for ids outside the table."""
-    import torch
     name = "mt_op_embedding"
     dt, gpu = _act_type(name, precision), table.get_device()
     (n,), (v, h) = _dims(name, "ids", ids, 1), _dims(name, "table", table, 2)
     _check(name, "table", table, (v, h), dt, gpu)
-    _check(name, "ids", ids, (n,), torch.int32, gpu)
+    _check(name, "ids", ids, (n,), _t().int32, gpu)
     if out is None:
-        out = torch.empty((n, h), dtype=dt, device=table.device)
+        out = table.new_empty((n, h))
     else:
         _check(name, "out", out, (n, h), dt, gpu)
     _run(name, gpu, 0, lambda work, size, stream: lib().mt_op_embedding(
@@ -747,7 +758,7 @@ def op_embedding(precision, table, ids, scale=1.0, out=None):
 def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add_to=None):
     """mt_op_embedding_grad: the gradient of op_embedding's table [vocab][hidden] (float32 with out_f32); `add_to`: a float32 gradient that it is added
     to instead."""
-    import torch
+    torch = _t()
     name = "mt_op_embedding_grad"
     dt, gpu = _act_type(name, precision), grad.get_device()
     (n, h), (m,) = _dims(name, "grad", grad, 2), _dims(name, "ids", ids, 1)
