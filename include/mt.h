@@ -443,7 +443,7 @@ int mt_op_layernorm(const float* d_x, const float* d_gamma, const float* d_beta,
  * workspace holds nothing between calls, and calls that may overlap need one each.  hip_stream belongs to the current device.  No atomics on
  * sums: equal inputs give equal bits.  Errors: NULL, CONFIG, SHAPE (also: a workspace smaller than the *_work function says), HIP.
  */
-/* Attention over n_seqs packed sequences.  Sequence b owns query rows d_q_start[b] .. d_q_start[b+1]-1 and key rows d_k_start[b] .. d_k_start[b+1]-1
+/* Attention over n_seqs (at most 16384) packed sequences.   Sequence b owns query rows d_q_start[b] .. d_q_start[b+1]-1 and key rows d_k_start[b] .. d_k_start[b+1]-1
  * (device int32 [n_seqs + 1], not falling; starts outside [0, total] are brought inside; d_k_start NULL: the queries').  With Lq queries and Lk keys,
  * query i sees all Lk keys or, causal, the keys j <= i + Lk - Lq: the last query sees the last key, so a single token is a sequence of one query, and a
  * prompt one of as many queries as keys.  Query head a reads key head a / (heads / kv_heads); heads % kv_heads == 0.
@@ -474,7 +474,7 @@ size_t mt_op_packed_attention_work(const mt_packed_attention* op, int32_t grad);
 
 /* Softmax cross entropy of z = x W^T over a vocabulary, which never stores z.  d_x [tokens][ldx], d_W [vocab][ldw], hidden columns each (a multiple of
  * 64); d_labels int32 [tokens]:  lse_i = log sum_v exp z_iv, loss_i = lse_i - z_i,label  (float32 [tokens], not averaged).  A label outside
- * [0, vocab) means none: its token's row is not read, its loss and lse are 0, its gradient is 0. */
+ * [0, vocab) means none: its token's row reaches nothing, whatever it holds; its loss, lse and gradient are 0.  vocab at most 2^22, tokens 2^23. */
 int mt_op_vocab_loss(int32_t precision, const void* d_x, int64_t ldx, const void* d_W, int64_t ldw, const int32_t* d_labels, float* d_loss, float* d_lse,
                      int32_t tokens, int32_t hidden, int32_t vocab, void* d_work, size_t work_bytes, void* hip_stream);
 /* dz_iv = weight_i (exp(z_iv - lse_i) - [v = label_i]), d_grad_x = dz W [tokens][hidden], d_grad_W = dz^T x [vocab][hidden] (dense, written whole;
@@ -488,7 +488,7 @@ size_t mt_op_vocab_loss_work(int32_t precision, int32_t tokens, int32_t hidden, 
 /* out_i = scale * table[id_i]; an id outside [0, vocab): a row of zeros.  hidden: a multiple of 8 (float32: of 4).  d_table [vocab][ldt], d_out [n][ldo]. */
 int mt_op_embedding(int32_t precision, const void* d_table, int64_t ldt, const int32_t* d_ids, float scale, void* d_out, int64_t ldo, int32_t n,
                     int32_t vocab, int32_t hidden, void* hip_stream);
-/* The table's gradient: d_grad_table[v] = scale * sum over i with id_i = v of d_grad[i], float32 sums; zeros for rows without a token.
+/* The table's gradient (n at most 2^24): d_grad_table[v] = scale * sum over i with id_i = v of d_grad[i], float32 sums; zeros for rows without a token.
  * out_f32 != 0 stores float32; accumulate != 0 (float32 only) adds to what is there instead and leaves other rows alone (a table that is also the
  * classifier's weights: mt_op_vocab_loss_grad with grad_W_f32 first, then this). */
 int mt_op_embedding_grad(int32_t precision, const void* d_grad, int64_t ldg, const int32_t* d_ids, float scale, void* d_grad_table, int64_t ldt,

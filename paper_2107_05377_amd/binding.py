@@ -685,6 +685,7 @@ def op_packed_attention(precision, q, k, v, q_start, k_start=None, causal=True, 
     [sequences + 1]; scale None: 1 / sqrt(width).  Returns the context [queries][heads][width] (`out`, or zeros where no sequence is) and with want_lse
     the statistics [heads][queries] float32 for the gradient (unspecified where no sequence is)."""
     torch = _t()
+    _dims("mt_op_packed_attention", "q", q, 3)
     ctx = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if want_lse else None
     _attention_call("mt_op_packed_attention", "mt_op_packed_attention", precision, q, k, v, q_start, k_start, causal, scale, ctx, lse)

@@ -961,7 +961,7 @@ hipError_t forward_with(const PackedAttn& p, const Deal& d, hipStream_t stream)
     static std::atomic<uint64_t> done{0};
     hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(packed_forward_kernel<E, DP, RW, KW, UB, STAGES>), F::LDS, done);
     if (e != hipSuccess) return e;
-    if (d.items * p.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (!fits_launch(d.items * p.kv_heads, F::NW * 64)) return hipErrorInvalidValue;
     packed_forward_kernel<E, DP, RW, KW, UB, STAGES><<<(unsigned)(d.items * p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
     if ((e = hipGetLastError()) != hipSuccess || d.keys_each == 0) return e;
     const int rows = std::min<int64_t>(F::BM, (int64_t)p.total_q * (p.heads / p.kv_heads));
@@ -995,7 +995,7 @@ hipError_t gradient_of(const PackedAttn& p, hipStream_t stream)
     if (e != hipSuccess) return e;
     float* stat = static_cast<float*>(p.work);
     const int64_t tiles_s = (int64_t)p.total_q * p.group / 128 + p.n_seqs, tiles_q = (int64_t)p.total_q * p.group / R::BM + p.n_seqs, tiles_k = (int64_t)p.total_k / G::BN + p.n_seqs;
-    if (tiles_q * p.kv_heads > 0x7FFFFFFF || tiles_k * p.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (!fits_launch(std::max({tiles_s, tiles_q, tiles_k}) * p.kv_heads, 256)) return hipErrorInvalidValue;
     packed_stat_kernel<E, DP><<<(unsigned)(tiles_s * p.kv_heads), 256, 0, stream>>>(p, stat);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     packed_dkv_kernel<E, DP, A, B, SK><<<(unsigned)(tiles_k * p.kv_heads), G::NW * 64, G::LDS, stream>>>(p, stat);

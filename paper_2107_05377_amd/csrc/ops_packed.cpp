@@ -23,11 +23,11 @@ bool apart(int64_t row, int64_t head, int32_t rows, int32_t heads, int32_t width
 }
 bool fits(const void* work, size_t have, size_t need) { return need == 0 || (work && ((uintptr_t)work & 255) == 0 && have >= need); }
 
-// sizes alone: MT_OK or what is wrong
+// sizes alone: MT_OK or what is wrong.  (Every workgroup looks through the sequences for its own: at 16384 of them for a tenth of a millisecond.)
 int attention_sizes(const mt_packed_attention* op)
 {
     if (!known(op->precision)) return MT_ERR_CONFIG;
-    if (op->n_seqs < 1 || op->n_seqs > 1 << 24 || op->heads < 1 || op->kv_heads < 1 || op->kv_heads > 65535 || op->heads % op->kv_heads != 0 || op->width < 8 ||
+    if (op->n_seqs < 1 || op->n_seqs > 16384 || op->heads < 1 || op->kv_heads < 1 || op->kv_heads > 65535 || op->heads % op->kv_heads != 0 || op->width < 8 ||
         op->width > 128 || op->width % 8 != 0 || op->total_q < 1 || op->total_k < 1 || !(op->scale > 0.f) || !std::isfinite(op->scale))
         return MT_ERR_SHAPE;
     // rows are numbered with 31 bits: a group's heads of all queries, and the keys, with room for a tile and for the longest shift between the two
@@ -133,7 +133,7 @@ int mt_op_packed_attention_grad(const mt_packed_attention* op, void* hip_stream)
 static int loss_sizes(int32_t precision, int32_t tokens, int32_t hidden, int32_t vocab)
 {
     if (!known(precision)) return MT_ERR_CONFIG;
-    if (tokens < 1 || tokens > 1 << 24 || hidden < 64 || hidden > 1 << 20 || hidden % 64 != 0 || vocab < 1 || vocab > 1 << 22) return MT_ERR_SHAPE;
+    if (tokens < 1 || tokens > 1 << 23 || hidden < 64 || hidden > 1 << 20 || hidden % 64 != 0 || vocab < 1 || vocab > 1 << 22) return MT_ERR_SHAPE;
     return MT_OK;
 }
 
@@ -199,6 +199,9 @@ int mt_op_vocab_loss_grad(int32_t precision, const void* d_x, int64_t ldx, const
     return result(launch_vocab_loss_grad(p, size == 4, static_cast<hipStream_t>(hip_stream)));
 }
 
+// tokens of a gradient: each workgroup of the sort adds up the counts of all, a quarter of a million loads at this many
+constexpr int32_t kMostSorted = 1 << 24;
+
 static int embedding_sizes(int32_t precision, int32_t n, int32_t vocab, int32_t hidden)
 {
     if (!known(precision)) return MT_ERR_CONFIG;
@@ -229,7 +232,7 @@ int mt_op_embedding(int32_t precision, const void* d_table, int64_t ldt, const i
 
 size_t mt_op_embedding_grad_work(int32_t precision, int32_t n, int32_t vocab, int32_t hidden)
 {
-    return embedding_sizes(precision, n, vocab, hidden) == MT_OK ? embedding_grad_work(n, vocab, hidden) : 0;
+    return embedding_sizes(precision, n, vocab, hidden) == MT_OK && n <= kMostSorted ? embedding_grad_work(n, vocab, hidden) : 0;
 }
 
 int mt_op_embedding_grad(int32_t precision, const void* d_grad, int64_t ldg, const int32_t* d_ids, float scale, void* d_grad_table, int64_t ldt,
@@ -238,6 +241,7 @@ int mt_op_embedding_grad(int32_t precision, const void* d_grad, int64_t ldg, con
     if (!d_grad || !d_ids || !d_grad_table) return MT_ERR_NULL;
     const int bad = embedding_sizes(precision, n, vocab, hidden);
     if (bad != MT_OK) return bad;
+    if (n > kMostSorted) return MT_ERR_SHAPE;
     const int size = precision == MT_BF16 ? 2 : 4, out_size = size == 4 || out_f32 ? 4 : 2;
     if (!at16(d_grad) || !at16(d_grad_table) || ldg < hidden || ldt < hidden || !rows16(ldg, size) || !rows16(ldt, out_size) || !std::isfinite(scale) ||
         (accumulate && out_size != 4) || !fits(d_work, work_bytes, embedding_grad_work(n, vocab, hidden)))

@@ -6,6 +6,9 @@
 
 namespace mt {
 
+// a launch has less than 2^32 threads
+inline bool fits_launch(int64_t groups, int threads) { return groups >= 0 && groups * threads < 1ll << 32; }
+
 // ---- attention over packed sequences.  Strides in elements; rows of a head are `d` contiguous elements.
 struct PackedAttn {
     const void *q, *k, *v;

@@ -582,7 +582,7 @@ hipError_t forward_of(const VocabLoss& p, hipStream_t stream)
         const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(vocab_stats_kernel<E, c.value>), P::LDS, done);
         if (e != hipSuccess) return e;
         const int64_t grid = (int64_t)((p.tokens + P::BN - 1) / P::BN) * ((p.vocab + P::BM - 1) / P::BM);
-        if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+        if (!fits_launch(grid, P::NT)) return hipErrorInvalidValue;
         vocab_stats_kernel<E, c.value><<<(unsigned)grid, P::NT, P::LDS, stream>>>(p, count, index, stats, at_label);
         return hipGetLastError();
     });
@@ -626,7 +626,7 @@ hipError_t gradient_of(const VocabLoss& p, hipStream_t stream)
             const int64_t grid_z = (int64_t)((p.tokens + PZ::BN - 1) / PZ::BN) * (width / PZ::BM);
             const int64_t tiles_x = (int64_t)((p.tokens + PX::BN - 1) / PX::BN) * ((p.hidden + PX::BM - 1) / PX::BM), grid_x = std::max<int64_t>(tiles_x, pl.ranges.blocks);
             const int64_t grid_w = (int64_t)((p.hidden + PW::BM - 1) / PW::BM) * ((width + PW::BN - 1) / PW::BN);
-            if (std::max({grid_z, grid_x, grid_w}) > 0x7FFFFFFF) return hipErrorInvalidValue;
+            if (!fits_launch(std::max({grid_z, grid_x, grid_w}), 512)) return hipErrorInvalidValue;
             vocab_dz_kernel<E, C><<<(unsigned)grid_z, PZ::NT, PZ::LDS, stream>>>(p, count, index, xc, v0, width, dz);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             vocab_dx_kernel<E, C><<<(unsigned)grid_x, PX::NT, PX::LDS, stream>>>(p, count, dz, v0, width, pl.ranges, part);

@@ -160,7 +160,8 @@ def test_attention_of_many_sequences(precision):
 
 @pytest.mark.parametrize("precision,heads,kv_heads,d,seqs,causal", [
     ("bf16", 4, 1, 64, [(1, 9001)], True), ("bf16", 4, 2, 128, [(2, 4097), (1, 100)], True), ("fp32", 2, 1, 64, [(1, 5003)], False),
-    ("bf16", 2, 1, 64, [(1111, 1111), (90, 1500)], True), ("bf16", 1, 1, 128, [(700, 1300)], False)])
+    ("bf16", 2, 1, 64, [(1111, 1111), (90, 1500)], True), ("bf16", 1, 1, 128, [(700, 1300)], False),
+    ("bf16", 128, 128, 16, [(2060, 2060)], True), ("bf16", 128, 128, 72, [(1700, 1701), (400, 400)], True), ("fp32", 128, 128, 8, [(2060, 2060)], False)])
 def test_attention_of_long_sequences(precision, heads, kv_heads, d, seqs, causal):
     check_attention(run_attention(precision, heads, kv_heads, d, seqs, causal))
 
@@ -282,7 +283,7 @@ def make_loss(precision, n, h, v, labelled, seed=0):
 
 @pytest.mark.parametrize("precision", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,h,v,labelled", [(1, 64, 1, 1.0), (1, 768, 1000, 1.0), (5, 64, 127, 1.0), (33, 128, 129, 0.5), (64, 192, 2051, 1.0), (129, 320, 500, 0.9),
-                                            (300, 768, 5003, 0.15), (1000, 64, 40, 0.7), (257, 1024, 4096, 1.0), (40, 64, 70, 0.0)])
+                                            (17, 64, 300, 0.5), (300, 768, 5003, 0.15), (1000, 64, 40, 0.7), (2100, 128, 8301, 0.9), (257, 1024, 4096, 1.0), (40, 64, 70, 0.0)])
 def test_vocab_loss(precision, n, h, v, labelled):
     print(f"vocab loss {precision} {n} x {h} x {v}", flush=True)
     p, dt, u = PRECISIONS[precision]
@@ -337,7 +338,7 @@ def test_vocab_loss_gradient_against_differences():
 
 @pytest.mark.parametrize("precision", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,h,v,kind", [(1, 8, 1, "any"), (61, 768, 30522, "words"), (500, 64, 37, "any"), (1025, 520, 300, "one"), (3000, 24, 5000, "words"),
-                                        (5000, 136, 100, "words"), (20011, 64, 1000, "one"), (33000, 72, 4000, "words"), (40000, 16, 70000, "any")])
+                                        (5000, 136, 100, "words"), (20011, 64, 1000, "one"), (33000, 72, 4000, "words"), (40000, 16, 70000, "any"), (140001, 8, 900, "words")])
 def test_embedding(precision, n, h, v, kind):
     print(f"embedding {precision} {n} x {h} of {v}, {kind}", flush=True)
     p, dt, u = PRECISIONS[precision]

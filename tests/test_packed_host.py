@@ -22,7 +22,7 @@ def attention(**change):
 @pytest.mark.parametrize("grad", [0, 1])
 @pytest.mark.parametrize("change,code", [
     ({"d_q": None}, mt.MT_ERR_NULL), ({"d_v": None}, mt.MT_ERR_NULL), ({"d_ctx": None}, mt.MT_ERR_NULL), ({"d_q_start": None}, mt.MT_ERR_NULL),
-    ({"precision": mt.MT_FP8_FFN}, mt.MT_ERR_CONFIG), ({"precision": 9}, mt.MT_ERR_CONFIG), ({"n_seqs": 0}, mt.MT_ERR_SHAPE),
+    ({"precision": mt.MT_FP8_FFN}, mt.MT_ERR_CONFIG), ({"precision": 9}, mt.MT_ERR_CONFIG), ({"n_seqs": 0}, mt.MT_ERR_SHAPE), ({"n_seqs": 16385}, mt.MT_ERR_SHAPE),
     ({"heads": 5}, mt.MT_ERR_SHAPE), ({"kv_heads": 0}, mt.MT_ERR_SHAPE), ({"width": 0}, mt.MT_ERR_SHAPE), ({"width": 60}, mt.MT_ERR_SHAPE),
     ({"width": 136}, mt.MT_ERR_SHAPE), ({"total_q": 0}, mt.MT_ERR_SHAPE), ({"total_k": -1}, mt.MT_ERR_SHAPE), ({"total_k": (1 << 29) + 1}, mt.MT_ERR_SHAPE),
     ({"total_q": (1 << 28) + 1}, mt.MT_ERR_SHAPE), ({"scale": 0.0}, mt.MT_ERR_SHAPE), ({"scale": -1.0}, mt.MT_ERR_SHAPE), ({"scale": float("nan")}, mt.MT_ERR_SHAPE),
@@ -53,7 +53,7 @@ def test_attention_results_and_workspaces():
 @pytest.mark.parametrize("change,code", [
     ({"x": None}, mt.MT_ERR_NULL), ({"W": None}, mt.MT_ERR_NULL), ({"labels": None}, mt.MT_ERR_NULL), ({"lse": None}, mt.MT_ERR_NULL),
     ({"precision": mt.MT_FP8_LAYER}, mt.MT_ERR_CONFIG), ({"tokens": 0}, mt.MT_ERR_SHAPE), ({"hidden": 96}, mt.MT_ERR_SHAPE), ({"hidden": 0}, mt.MT_ERR_SHAPE),
-    ({"vocab": 0}, mt.MT_ERR_SHAPE), ({"vocab": (1 << 22) + 1}, mt.MT_ERR_SHAPE), ({"x": FAKE + 2}, mt.MT_ERR_SHAPE), ({"ldx": 120}, mt.MT_ERR_SHAPE),
+    ({"vocab": 0}, mt.MT_ERR_SHAPE), ({"vocab": (1 << 22) + 1}, mt.MT_ERR_SHAPE), ({"tokens": (1 << 23) + 1}, mt.MT_ERR_SHAPE), ({"x": FAKE + 2}, mt.MT_ERR_SHAPE), ({"ldx": 120}, mt.MT_ERR_SHAPE),
     ({"ldw": 132}, mt.MT_ERR_SHAPE), ({"work": None}, mt.MT_ERR_SHAPE), ({"work": FAKE + 128}, mt.MT_ERR_SHAPE), ({"bytes": -1}, mt.MT_ERR_SHAPE)])
 def test_vocab_loss_refusals(change, code):
     L = mt.lib()
@@ -87,7 +87,7 @@ def test_embedding_refusals():
     for bad in (dict(n=0), dict(vocab=0), dict(hidden=60), dict(hidden=0), dict(scale=float("nan"))):
         assert look(**bad) == grad(**bad) == mt.MT_ERR_SHAPE
     assert look(ldt=56) == look(ldo=68) == look(table=FAKE + 4) == look(out=FAKE + 8) == mt.MT_ERR_SHAPE
-    assert grad(ldg=0) == grad(ldt=68) == grad(out=FAKE + 4) == grad(add=1) == mt.MT_ERR_SHAPE            # (adding needs float32)
+    assert grad(n=(1 << 24) + 1) == grad(ldg=0) == grad(ldt=68) == grad(out=FAKE + 4) == grad(add=1) == mt.MT_ERR_SHAPE            # (adding needs float32)
 
 
 def test_work_sizes_of_the_largest_calls_fit_their_type():
