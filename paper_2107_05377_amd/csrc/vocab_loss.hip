@@ -232,6 +232,43 @@ struct Product {
     }
 };
 
+// A workgroup's block to memory, row b (a lane's) of the block at row_at(b) (null: nowhere), its first `cols` columns.  The accumulators hold 4 columns of 32
+// rows per instruction, which memory would see as 32 pieces of 16 bytes; through the idle ring they become whole rows, 16 bytes a lane.
+template <typename P, typename Out, bool ADD, typename RowAt>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::tmi][P::tni], unsigned char* lds, int cols, RowAt row_at)
+{
+    typedef Out out4 __attribute__((ext_vector_type(4)));
+    typedef Out out16 __attribute__((ext_vector_type(16 / sizeof(Out))));
+    constexpr int ROWB = P::BM * sizeof(Out), LANES = ROWB / 16, ROWS = P::BN / P::tni, PER = 16 / sizeof(Out);
+    static_assert(ROWS * ROWB <= P::LDS && P::NT % LANES == 0 && LANES >= 16, "");
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, c = threadIdx.x % LANES;
+    const int mine = P::wave_n() / P::tni + l32;
+#pragma unroll
+    for (int j = 0; j < P::tni; ++j) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < P::tmi; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = (P::wave_m() + i * 32 + 8 * q + 4 * half) * (int)sizeof(Out);
+                out4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (Out)acc[i][j][4 * q + e];
+                *reinterpret_cast<out4*>(lds + mine * ROWB + (((at >> 4) ^ (mine & 15)) << 4) + (at & 15)) = o;
+            }
+        __syncthreads();
+#pragma unroll 4
+        for (int r = threadIdx.x / LANES; r < ROWS; r += P::NT / LANES) {
+            Out* row = row_at((r >> 5) * (P::tni * 32) + j * 32 + (r & 31));
+            if (!row || c * PER >= cols) continue;
+            out16 v = *reinterpret_cast<const out16*>(lds + r * ROWB + ((c ^ (r & 15)) << 4));
+            out16* to = reinterpret_cast<out16*>(row + c * PER);
+            if constexpr (ADD) v += *to;
+            *to = v;
+        }
+    }
+}
+
 // Workgroup id -> block of a grid of m x n: consecutive ids go to the 8 XCDs in turn, so each gets a run of blocks of its own, which walks bands of
 // kBand blocks of m and shares their operands in that XCD's L2.
 constexpr int kBand = 8;
@@ -378,25 +415,28 @@ __global__ __launch_bounds__((Pick<E, false, false, C>::P::NT)) void vocab_dz_ke
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int vb = v0 + P::wave_m(), tb = t0 + P::wave_n();
     const int n_pad = (n + 63) & ~63;
+    // straight from the accumulators, 8 bytes a lane: the exponentials between the stores leave them time (through LDS as whole rows: 3 % slower)
 #pragma unroll
     for (int j = 0; j < P::tni; ++j) {
         const int t = tb + j * 32 + l32;
         if (t >= n_pad) continue;
         const bool real = t < n;
-        const int at = real ? index[t] : 0, label = real ? p.labels[at] : -1;
+        const int at = real ? index[t] : 0, label = (real ? p.labels[at] : -1) - vb - 4 * half;
         const float lse = real ? p.lse[at] * kLog2e : 0.f, g = real ? p.weight[at] : 0.f;
+        typename E::elem* row = dz + (int64_t)t * width + vb - piece0 + 4 * half;
 #pragma unroll
         for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int v = vb + i * 32 + 8 * q + 4 * half;
+                const int v = i * 32 + 8 * q;
                 out4 o;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], kLog2e, -lse)) - (v + e == label ? 1.f : 0.f);
-                    o[e] = (typename E::elem)(real && v + e < p.vocab ? w * g : 0.f);
+                    float w = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], kLog2e, -lse));
+                    w = v + e == label ? w - 1.f : w;
+                    o[e] = (typename E::elem)(real && vb + 4 * half + v + e < p.vocab ? w * g : 0.f);
                 }
-                *reinterpret_cast<out4*>(dz + (int64_t)t * width + v - piece0) = o;
+                *reinterpret_cast<out4*>(row + v) = o;
             }
     }
 }
@@ -428,25 +468,9 @@ __global__ __launch_bounds__((Pick<E, true, false, C>::P::NT)) void vocab_dx_ker
     f32x16 acc[P::tmi][P::tni];
     const auto* w = static_cast<const typename E::elem*>(p.w) + (int64_t)piece0 * p.ldw;
     P::run(acc, Operand{w, p.ldw, nullptr, p.hidden, p.vocab - piece0}, h0, Operand{dz, width, nullptr, n, 0}, t0, k0, k1, lds);
-    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-#pragma unroll
-    for (int j = 0; j < P::tni; ++j) {
-        const int t = t0 + P::wave_n() + j * 32 + l32;
-        if (t >= n) continue;
-#pragma unroll
-        for (int i = 0; i < P::tmi; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int h = h0 + P::wave_m() + i * 32 + 8 * q + 4 * half;
-                if (h >= p.hidden) continue;
-                f32x4* at = reinterpret_cast<f32x4*>(part + ((int64_t)split * n + t) * p.hidden + h);
-                f32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-                if (piece0 > 0) v += *at;
-                *at = v;
-            }
-    }
+    const auto row_at = [&](int b) { return t0 + b < n ? part + ((int64_t)split * n + t0 + b) * p.hidden + h0 : nullptr; };
+    if (piece0 > 0) store_rows<P, float, true>(acc, lds, p.hidden - h0, row_at);
+    else store_rows<P, float, false>(acc, lds, p.hidden - h0, row_at);
 }
 
 // dW of one piece: the sum over the labelled tokens
@@ -455,7 +479,6 @@ __global__ __launch_bounds__((Pick<E, true, true, C>::P::NT)) void vocab_dw_kern
                                                                                    const typename E::elem* xc, int piece0, int width)
 {
     typedef typename Pick<E, true, true, C>::P P;
-    typedef Out out4 __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int n = *count, h_blocks = (p.hidden + P::BM - 1) / P::BM, v_blocks = (width + P::BN - 1) / P::BN;
     int bh, bv;
@@ -463,23 +486,8 @@ __global__ __launch_bounds__((Pick<E, true, true, C>::P::NT)) void vocab_dw_kern
     const int h0 = bh * P::BM, v0 = bv * P::BN;
     f32x16 acc[P::tmi][P::tni];
     P::run(acc, Operand{xc, p.hidden, nullptr, p.hidden, n}, h0, Operand{dz, width, nullptr, width, (n + 63) & ~63}, v0, 0, n, lds);
-    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-#pragma unroll
-    for (int j = 0; j < P::tni; ++j) {
-        const int v = piece0 + v0 + P::wave_n() + j * 32 + l32;
-        if (v >= min(p.vocab, piece0 + width)) continue;
-#pragma unroll
-        for (int i = 0; i < P::tmi; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int h = h0 + P::wave_m() + i * 32 + 8 * q + 4 * half;
-                if (h >= p.hidden) continue;
-                out4 o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (Out)acc[i][j][4 * q + e];
-                *reinterpret_cast<out4*>(static_cast<Out*>(p.dw) + (int64_t)v * p.hidden + h) = o;
-            }
-    }
+    const int rows = min(p.vocab - piece0, width) - v0;
+    store_rows<P, Out, false>(acc, lds, p.hidden - h0, [&](int b) { return b < rows ? static_cast<Out*>(p.dw) + (int64_t)(piece0 + v0 + b) * p.hidden + h0 : nullptr; });
 }
 
 // dx: the ranges' sums put together and rounded, in the tokens' places; zeros for tokens without a label.  A workgroup a row.
