@@ -927,7 +927,18 @@ __global__ __launch_bounds__(KW * RW * 64, (Tile<E, DP>::ROWB == 128 ? 2 : 1)) v
 }
 
 // ---- launches
-// How the rows of the forward pass are dealt out.
+// How the rows of the forward pass are dealt out, by what is known on the host: the sums of the lengths, not the lengths.  Measured on both sides (bfloat16,
+// us; q: queries of a sequence, k: its keys, D: columns of a head):
+//   32 rows, four wavefronts (D = 128: two) that share the keys, for rows of one query.  With 64 rows and two of them instead: 128 x 12 heads of D = 64 with
+//     20..61 keys 14.2, not 19.8; 200..500 keys 30.4, not 32.3; 1000..2000 keys 111, not 110; 300 x 4 key heads of D = 128 with 1000..3000 keys 222, not 218;
+//     float32 with 200..500 keys 111, not 101.  Hence from 256 keys per sequence on, and always with few workgroups, whose keys may be dealt out (below),
+//     because a long sequence among short ones would hold up the launch: short ones alone (64 sequences of 8..28 keys) would take 10.3, not 12.5.
+//   64 rows, two wavefronts of rows by two that share the keys, for short sequences (20..60 tokens 9.8; 128 rows 10.8) and few tiles (512 tokens x 4, four
+//     key heads 12.1; 14.2.  1000 tokens, twelve 16.7; 21.0.  1000 tokens, eight of D = 128 with groups of 4 23.6; 30.6).
+//   128 rows, four wavefronts, each with its own rows and all the keys, so that each key block is read from LDS for twice the rows: 512 tokens x 8, four key
+//     heads 16.0; 64 rows 19.4.  256 x 64 tokens, twelve heads 31.4; 35.1, 256 x 30..80 36; 38.  64 x 128 tokens, twelve heads, 15.1; 19.6.  9 sequences of 300..4001 tokens 111; 131.  8192 tokens, D = 128 560; 698.
+//   Keys dealt out to several workgroups, whose sums a second launch joins: one token over 8192 keys, eight heads 17.5; not dealt out 114.
+//     32 tokens over 100..8191 keys 33.8; 115.
 struct Deal {
     int rows_each;          // rows of a workgroup: 32, 64 or 128
     int keys_each;          // > 0: keys of a workgroup
@@ -938,12 +949,13 @@ Deal deal_of(int n_seqs, int total_q, int total_k, int heads, int kv_heads)
     const int64_t group = heads / kv_heads, rows = total_q * group;
     Deal d{128, 0, 0, 0};
     const auto tiles = [&](int bm) { return rows / bm + n_seqs; };
-    if (rows <= 32ll * n_seqs) d.rows_each = 32;
-    else if (rows <= 96ll * n_seqs || tiles(128) * kv_heads < 2048) d.rows_each = 64;
+    const bool few = tiles(32) * kv_heads < 1024;
+    if (rows <= 32ll * n_seqs && (few || total_k > 256ll * n_seqs)) d.rows_each = 32;
+    else if (rows <= 40ll * n_seqs || tiles(128) * kv_heads < 512) d.rows_each = 64;
     d.tiles = tiles(d.rows_each);
     d.items = d.tiles;
-    if (d.rows_each == 32 && d.tiles * kv_heads < 1024) {
-        // few workgroups: keys dealt out so that there are about 1024, 256 keys each at least (what a workgroup needs to get going costs as much)
+    if (d.rows_each == 32 && few) {
+        // about 1024 workgroups of 512 keys each at least (what a workgroup needs to get going costs as much as 256 keys)
         const int64_t each = std::max<int64_t>(512, ((int64_t)total_k * kv_heads / 1024 + 255) / 256 * 256);
         if (total_k > each) {
             d.keys_each = (int)each;

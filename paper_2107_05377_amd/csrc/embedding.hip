@@ -59,6 +59,8 @@ struct SortPass {
     int32_t* hist;                  // [workgroups][256]
     int n, vocab, shift, bits;
 };
+// up to 4096 tokens (what one workgroup's LDS holds twice) are sorted by one launch: 1000 tokens of width 768, whole gradient 25.7 us, with the launches of the long
+// sort 31.5; 4096 tokens 28.7 and 34.0
 constexpr int kSmallSort = 4096;
 
 __device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i)
@@ -394,7 +396,8 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(Embedding p, Sums s
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 int chunks_of(int n) { return (n + kChunk - 1) / kChunk; }
-// keys of a workgroup of the sort: enough workgroups to spread, few enough that each can add up all counts
+// keys of a thread of the sort: 4 spread the work over more workgroups, but each adds up the counts of all.  Whole gradient with 4 and with 16: 32768 tokens 39.3 and
+// 60.6 us, 131072 60.2 and 76.6, 400000 128.7 and 122.6
 int items_of(int n) { return n <= 1 << 17 ? 4 : 16; }
 int sort_groups(int n) { return (n + 256 * items_of(n) - 1) / (256 * items_of(n)); }
 

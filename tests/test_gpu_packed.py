@@ -156,6 +156,14 @@ def test_attention(precision, heads, kv_heads, d, seqs, causal, layout):
 def test_attention_of_many_sequences(precision):
     check_attention(run_attention(precision, 2, 1, 64, [(i % 5, i % 5) for i in range(150)], True))
     check_attention(run_attention(precision, 2, 2, 64, [(1, 1 + i % 9) for i in range(65)], True))
+    check_attention(run_attention(precision, 64, 64, 16, [(1, 1 + i % 40) for i in range(40)], True, "heads"))
+    check_attention(run_attention(precision, 128, 64, 16, [(1, 150 + 70 * (i % 9)) for i in range(20)], True))
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,d,seqs,causal", [(128, 64, 64, MIXED, True), (64, 64, 40, MIXED, False), (256, 64, 128, CACHED, True), (256, 64, 24, EMPTY, True)])
+def test_attention_of_many_heads(precision, heads, kv_heads, d, seqs, causal):
+    check_attention(run_attention(precision, heads, kv_heads, d, seqs, causal, before=2, behind=1))
 
 
 @pytest.mark.parametrize("precision,heads,kv_heads,d,seqs,causal", [
@@ -283,7 +291,8 @@ def make_loss(precision, n, h, v, labelled, seed=0):
 
 @pytest.mark.parametrize("precision", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,h,v,labelled", [(1, 64, 1, 1.0), (1, 768, 1000, 1.0), (5, 64, 127, 1.0), (33, 128, 129, 0.5), (64, 192, 2051, 1.0), (129, 320, 500, 0.9),
-                                            (17, 64, 300, 0.5), (300, 768, 5003, 0.15), (1000, 64, 40, 0.7), (2100, 128, 8301, 0.9), (257, 1024, 4096, 1.0), (40, 64, 70, 0.0)])
+                                            (17, 64, 300, 0.5), (300, 768, 5003, 0.15), (1000, 64, 40, 0.7), (2100, 128, 8301, 0.9), (257, 1024, 4096, 1.0), (40, 64, 70, 0.0),
+                                            (64, 128, 1000, 0.8), (34, 64, 515, 1.0), (65, 64, 700, 0.9)])
 def test_vocab_loss(precision, n, h, v, labelled):
     print(f"vocab loss {precision} {n} x {h} x {v}", flush=True)
     p, dt, u = PRECISIONS[precision]
