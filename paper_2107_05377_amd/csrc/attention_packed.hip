@@ -552,13 +552,14 @@ __global__ __launch_bounds__(RW * KW * 64, (waves_of<E, DP>(UB == 1 ? 3 : 2))) v
 
 // the chunks of a tile's keys put together, one workgroup per 4 rows of a tile and key head: 64 lanes a row
 template <typename E, int DP, int BM>
-__global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys_each)
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn p, int keys_each, int items)
 {
     typedef typename E::elem elem;
     constexpr int ROW = DP + 4, COLS = DP / 64;
     const int group = p.group, item = __builtin_amdgcn_readfirstlane(blockIdx.x / p.kv_heads), kvh = blockIdx.x - item * p.kv_heads;
     Seq s;
     if (!find_tile<4, false, true>(p, item, group, BM, keys_each, s) || s.chunks == 1) return;
+    if (s.first < 0 || (int64_t)s.first + s.chunks > items) return;        // starts that fall name more items than there are
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int rows = s.lq * group, tiles = (rows + BM - 1) / BM, r = blockIdx.y * 4 + wave, row = (tiles - 1 - s.tile) * BM + r;
     if (row >= rows) return;
@@ -990,7 +991,7 @@ hipError_t forward_with(const PackedAttn& p, const Deal& d, hipStream_t stream)
     packed_forward_kernel<E, DP, RW, KW, UB, STAGES><<<(unsigned)(d.items * p.kv_heads), F::NW * 64, F::LDS, stream>>>(p, d.keys_each);
     if ((e = hipGetLastError()) != hipSuccess || d.keys_each == 0) return e;
     const int rows = std::min<int64_t>(F::BM, (int64_t)p.total_q * (p.heads / p.kv_heads));
-    packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)(d.tiles * p.kv_heads), (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each);
+    packed_join_kernel<E, DP, F::BM><<<dim3((unsigned)(d.tiles * p.kv_heads), (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(p, d.keys_each, (int)d.items);
     return hipGetLastError();
 }
 // (rings of at most 64 KB, of which a compute unit holds two, as long as that leaves two stages)

@@ -175,6 +175,17 @@ def test_attention_of_long_sequences(precision, heads, kv_heads, d, seqs, causal
 
 
 @pytest.mark.parametrize("precision", ["bf16", "fp32"])
+def test_attention_of_starts_that_fall(precision):
+    """Starts that fall name more chunks of keys than the workspace holds: those are left out, the first sequence is as if it were alone."""
+    p, dt, _ = PRECISIONS[precision]
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    q, k, v = normal(gen, 1, 4, 64, dtype=dt), normal(gen, 9001, 1, 64, dtype=dt), normal(gen, 9001, 1, 64, dtype=dt)
+    qs, ks = torch.tensor([0, 1, 0, 1, 0, 1], dtype=torch.int32, device="cuda"), torch.tensor([0, 9001, 0, 9001, 0, 9001], dtype=torch.int32, device="cuda")
+    got, alone = mt.op_packed_attention(p, q, k, v, qs, ks), mt.op_packed_attention(p, q, k, v, qs[:2], ks[:2])
+    assert torch.equal(got, alone)
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
 def test_attention_of_large_scores(precision):
     """Scores of +-100 and more: weights of 0 and 1, a maximum that rises from tile to tile."""
     p, dt, _ = PRECISIONS[precision]
