@@ -34,6 +34,19 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base) : "m0");
 }
+// both with the lanes of `on` alone (one at least), which the compiler need not know: what it has to do about other lanes would cost it a branch a load
+__device__ __forceinline__ void load_to_lds_of(uint64_t on, const void* from, uint32_t to)
+{
+    uint64_t all;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b64 exec, %0"
+                 : "=&s"(all) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(on) : "m0");
+}
+__device__ __forceinline__ void load_to_lds_of(uint64_t on, const void* base, uint32_t offset, uint32_t to)
+{
+    uint64_t all;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b64 exec, %0"
+                 : "=&s"(all) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base), "s"(on) : "m0");
+}
 // the same with 4 bytes a lane
 __device__ __forceinline__ void load_to_lds_4(const void* from, uint32_t to)
 {

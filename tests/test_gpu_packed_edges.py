@@ -1,0 +1,52 @@
+"""The operators on packed tokens at the edges of what their description allows.  Formulas, bounds and helpers are those of test_gpu_packed."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2107_05377_amd as mt  # noqa: E402
+import test_gpu_packed as base  # noqa: E402
+from test_gpu_packed import PRECISIONS, normal, starts, within  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    mt.lib()
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,d,length", [(2, 1, 64, 50), (2, 1, 80, 50), (3, 1, 8, 70), (2, 2, 24, 300), (4, 1, 72, 200), (1, 1, 120, 33)])
+def test_attention_key_of_minus_infinity_at_any_width(precision, heads, kv_heads, d, length):
+    """A key whose score is -infinity has weight 0: the result is that without the key, at whatever width.  (0 times -infinity makes the column of dq NaN in
+    which the key is infinite, by the formula.)"""
+    p, dt, u = PRECISIONS[precision]
+    print(f"attention {precision} {heads}/{kv_heads} x {d}, a key of -infinity among {length}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(d + length)
+    q, g = normal(gen, length, heads, d, dtype=dt), normal(gen, length, heads, d, dtype=dt)
+    k, v = normal(gen, length, kv_heads, d, dtype=dt), normal(gen, length, kv_heads, d, dtype=dt)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    bad = length // 3
+    rest = [i for i in range(length) if i != bad]
+    k[bad, :, 0] = -math.inf
+    scale = 1 / math.sqrt(d)
+    want, bound = base.attention_formula(q, k[rest].contiguous(), v[rest].contiguous(), g, [0, length], [0, length - 1], False, scale, u)
+    qs = starts([length])
+    ctx, lse = mt.op_packed_attention(p, q, k, v, qs, causal=False, want_lse=True)
+    within(ctx, want["ctx"], bound["ctx"], "ctx")
+    assert ((lse.double() - want["lse"]).abs() <= bound["lse"]).all()
+    dq, dk, dv = mt.op_packed_attention_grad(p, g, q, k, v, ctx, lse, qs, causal=False)
+    within(dq[..., 1:], want["dq"][..., 1:], bound["dq"][..., 1:], "dq")
+    assert torch.isnan(dq[..., 0]).all()
+    for name, got in (("dk", dk), ("dv", dv)):
+        within(got[rest], want[name], bound[name], name)
+        assert (got[bad] == 0).all(), name
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("heads,d,length", [(1, 8, 50), (5, 24, 150), (3, 80, 150), (2, 104, 70)])
+def test_attention_keys_not_seen_reach_nothing_at_any_width(precision, value, heads, d, length):
+    base.test_attention_keys_not_seen_reach_nothing(precision, value, heads, d, length)
