@@ -135,11 +135,21 @@ __device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsign
 }
 
 // ---- sequences
+constexpr int kTilesFree = 4;       // tiles of a sequence whose keys are dealt out without regard to the others'
 struct Seq {
     int q0, lq, k0, lk, tile;
     int chunk, chunks, first;       // of keys: this one's, how many the sequence has, the number of the tile's first item
 };
 __device__ __forceinline__ int clamp_start(int v, int total) { return min(max(v, 0), total); }
+
+// Chunks of a sequence's keys: of `each` keys (a multiple of 256), but no more than the sequence's part of the workgroups that there are (Deal::items) gives each
+// of its tiles; then they are longer.
+__device__ __forceinline__ int chunks_of(int lk, int tiles, int each)
+{
+    const int n = max(1, (lk + each - 1) / each);
+    return tiles > kTilesFree ? min(n, 1 + lk / (each / kTilesFree) / tiles) : n;       // (up to kTilesFree tiles the part is never less than n)
+}
+__device__ __forceinline__ int chunk_keys(int lk, int chunks, int each) { return chunks * each >= lk ? each : ((lk + chunks - 1) / chunks + 255) / 256 * 256; }
 
 // Workgroups: key heads first, so that the tiles of a sequence, whose cost falls from the first to the last, end a launch with the cheapest, and a key head's
 // workgroups share an XCD where there are 8 key heads or a part of 8.
@@ -151,7 +161,7 @@ __device__ __forceinline__ Seq same_in_all(const Seq& s)
 }
 
 // Item w of a list: for every sequence its tiles (`tile` rows each, `per` rows per token, of the queries or of the keys), and for every tile with
-// keys_each > 0 its sequence's chunks of that many keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are
+// keys_each > 0 its sequence's chunks of about that many keys.  BY_TILE: w counts tiles, chunk is 0.  False behind the last.  Starts outside the arrays are
 // brought inside, a sequence that would end before it starts is empty.  A workgroup looks through 64 sequences for each of its wavefronts at a time:
 // one load and a prefix sum, about a microsecond in which nothing else happens.
 template <int NW, bool KEYS, bool BY_TILE = false>
@@ -166,7 +176,7 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& p, int w, int per, i
         const int q0 = clamp_start(p.q_start[b], p.total_q), lq = max(clamp_start(p.q_start[b + 1], p.total_q) - q0, 0);
         const int k0 = clamp_start(p.k_start[b], p.total_k), lk = max(clamp_start(p.k_start[b + 1], p.total_k) - k0, 0);
         const int tiles = mine_b < p.n_seqs ? (int)(((int64_t)(KEYS ? lk : lq) * per + tile - 1) / tile) : 0;
-        const int chunks = keys_each > 0 ? max(1, (lk + keys_each - 1) / keys_each) : 1;
+        const int chunks = keys_each > 0 ? chunks_of(lk, tiles, keys_each) : 1;
         if (!BY_TILE && keys_each == 0 && p.n_seqs > 1 && p.n_seqs <= 64) {
             // few sequences: the tiles that are followed by most others of their sequence first, in all sequences (the longest sequence last in the
             // list would otherwise end the launch with its longest tiles).  behind(d): tiles followed by d others or more.
@@ -430,8 +440,9 @@ __global__ __launch_bounds__(RW * KW * 64, (waves_of<E, DP>(UB == 1 ? 3 : 2))) v
     const int limit = limit_of(my_row), wave_min = limit_all(r0 + rw * 32), wave_max = limit_all(r0 + rw * 32 + 31);
     int n_keys = limit_all(r0 + BM - 1) + 1, t0 = 0;
     if (keys_each > 0) {
-        t0 = s.chunk * (keys_each / TK);
-        n_keys = min(n_keys, (s.chunk + 1) * keys_each);
+        const int each = chunk_keys(s.lk, s.chunks, keys_each);
+        t0 = s.chunk * (each / TK);
+        n_keys = min(n_keys, (s.chunk + 1) * each);
     }
     const int n_tiles = n_keys > 0 ? (n_keys + TK - 1) / TK : 0;
 
@@ -997,8 +1008,11 @@ Deal deal_of(int n_seqs, int total_q, int total_k, int heads, int kv_heads)
         const int64_t each = std::max<int64_t>(512, ((int64_t)total_k * kv_heads / 1024 + 255) / 256 * 256);
         if (total_k > each) {
             d.keys_each = (int)each;
-            // sum over sequences of (rows / 32 + 1) (keys / each + 1)
-            d.items = (rows / 32) * (total_k / each) + rows / 32 + total_k / each + n_seqs;
+            // The host knows sums alone.  A sequence's tiles are t <= rows / 32 + 1, its chunks c <= 1 + keys / each, and t (c - 1) <= keys / (each / 4), which
+            // chunks_of sees to: without that only the product of the sums would bound them, half a million workgroups and 8 GB for 500 tokens of 32 heads
+            // on one, of which 1000 had anything to do.  So there are at most 5120, and 87 MB.
+            const int64_t c = total_k / each;
+            d.items = d.tiles + std::min((rows / 32 + 1) * c, total_k / (each / kTilesFree));
         }
     }
     return d;

@@ -50,3 +50,14 @@ def test_attention_key_of_minus_infinity_at_any_width(precision, heads, kv_heads
 @pytest.mark.parametrize("heads,d,length", [(1, 8, 50), (5, 24, 150), (3, 80, 150), (2, 104, 70)])
 def test_attention_keys_not_seen_reach_nothing_at_any_width(precision, value, heads, d, length):
     base.test_attention_keys_not_seen_reach_nothing(precision, value, heads, d, length)
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,count", [(64, 100), (128, 300)])
+def test_attention_of_long_prompts_among_single_tokens(precision, causal, d, count):
+    """Keys dealt out to workgroups where two sequences have many tiles of rows, whose chunks are then fewer and longer than those of the others (3 of 1536 keys and
+    1 of all 4000 instead of 8 of 512), and sequences without keys or queries."""
+    seqs = [(1, 300 + 41 * (i % 23)) for i in range(count)]
+    seqs[count // 2], seqs[count - 20], seqs[3], seqs[70] = (160, 4000), (48, 4000), (1, 0), (0, 600)
+    base.check_attention(base.run_attention(precision, 8, 1, d, seqs, causal, before=2, behind=3))
