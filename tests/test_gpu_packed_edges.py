@@ -61,3 +61,18 @@ def test_attention_of_long_prompts_among_single_tokens(precision, causal, d, cou
     seqs = [(1, 300 + 41 * (i % 23)) for i in range(count)]
     seqs[count // 2], seqs[count - 20], seqs[3], seqs[70] = (160, 4000), (48, 4000), (1, 0), (0, 600)
     base.check_attention(base.run_attention(precision, 8, 1, d, seqs, causal, before=2, behind=3))
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,d,seqs", [
+    (1, 1, 64, [(i % 5, i % 5) for i in range(1100)]), (2, 1, 128, [(i % 7, i % 6) for i in range(300)]), (1, 1, 80, [(i % 40, i % 45) for i in range(300)]),
+    (2, 1, 64, [(1, 1 + 37 * i % 1500) for i in range(600)]), (2, 2, 128, [(1, 1 + 37 * i % 900) for i in range(300)]), (1, 1, 16, [(1, i % 3) for i in range(1025)])])
+def test_attention_of_more_sequences_than_a_workgroup_looks_at_once(precision, heads, kv_heads, d, seqs):
+    base.check_attention(base.run_attention(precision, heads, kv_heads, d, seqs, True, before=1, behind=1))
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,d,length", [(96, 32, 24, 700), (80, 16, 64, 850), (48, 8, 128, 700)])
+def test_attention_of_groups_that_do_not_divide_a_tile(precision, heads, kv_heads, d, length):
+    """Groups of 3, 5 and 6 heads in calls large enough for 128 rows a workgroup."""
+    base.check_attention(base.run_attention(precision, heads, kv_heads, d, [(length, length), (33, 40)], True))
