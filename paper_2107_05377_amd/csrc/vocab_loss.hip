@@ -302,8 +302,11 @@ struct Pick<F32, A, B, FEW> { typedef Product<F32, A, B, 4, 1, 1, 1, 32, 4> P; }
 template <bool A, bool B>
 struct Pick<F32, A, B, MID> { typedef Product<F32, A, B, 2, 2, 2, 2, 32, 2> P; };
 
+// The reference is log2e times the largest z, as rounded, and nothing rounds between it and the exponents log2e z - ref (one fused operation): the loss, which is
+// their sum's logarithm less the label's exponent, is then good to a few 2^-24, where lse - z would be good to as many of lse, of which little is left over for
+// a token that the model is sure of.
 struct Stat {
-    float top, sum;         // sum of exp2(log2e (z - top))
+    float ref, sum;         // sum of exp2(log2e z - ref)
 };
 
 // ---- forward: a block of z (vocabulary in registers, tokens in lanes) -> a Stat per token and wavefront's range of the vocabulary
@@ -337,13 +340,13 @@ __global__ __launch_bounds__((Pick<E, false, false, C>::P::NT)) void vocab_stats
                 top = fmaxf(top, acc[i][j][e]);
             }
         top = lane_pair_max<32>(top);
-        const float from = top == -INFINITY ? 0.f : top * kLog2e;
+        const float ref = top * kLog2e, from = top == -INFINITY ? 0.f : ref;
 #pragma unroll
         for (int i = 0; i < P::tmi; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -from));
         sum = lane_pair_sum<32>(sum);
-        if (t < n && half == 0) stats[(int64_t)(vb / (P::tmi * 32)) * p.tokens + t] = Stat{top, sum};
+        if (t < n && half == 0) stats[(int64_t)(vb / (P::tmi * 32)) * p.tokens + t] = Stat{ref, sum};
     }
 }
 
@@ -364,30 +367,30 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabLoss p, const int3
         Stat v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = stats[(int64_t)min(r0 + k * SLICES, ranges - 1) * p.tokens + min(t, n - 1)];
-        float top = s.top;
+        float ref = s.ref;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) top = fmaxf(top, v[k].top);
-        const float from = top == -INFINITY ? 0.f : top;
-        s.sum *= __builtin_amdgcn_exp2f((s.top - from) * kLog2e);
+        for (int k = 0; k < 8; ++k) ref = fmaxf(ref, v[k].ref);
+        const float from = ref == -INFINITY ? 0.f : ref;
+        s.sum *= __builtin_amdgcn_exp2f(s.ref - from);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (r0 + k * SLICES < ranges) s.sum = fmaf(v[k].sum, __builtin_amdgcn_exp2f((v[k].top - from) * kLog2e), s.sum);
-        s.top = top;
+            if (r0 + k * SLICES < ranges) s.sum = fmaf(v[k].sum, __builtin_amdgcn_exp2f(v[k].ref - from), s.sum);
+        s.ref = ref;
     }
     part[slice][threadIdx.x % TOK] = s;
     __syncthreads();
     if (slice != 0 || !mine) return;
-    float top = -INFINITY;
+    float ref = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < SLICES; ++k) top = fmaxf(top, part[k][threadIdx.x].top);
-    const float from = top == -INFINITY ? 0.f : top;
+    for (int k = 0; k < SLICES; ++k) ref = fmaxf(ref, part[k][threadIdx.x].ref);
+    const float from = ref == -INFINITY ? 0.f : ref;
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < SLICES; ++k) sum = fmaf(part[k][threadIdx.x].sum, __builtin_amdgcn_exp2f((part[k][threadIdx.x].top - from) * kLog2e), sum);
-    const float lse = top + __builtin_amdgcn_logf(sum) * kLn2;
+    for (int k = 0; k < SLICES; ++k) sum = fmaf(part[k][threadIdx.x].sum, __builtin_amdgcn_exp2f(part[k][threadIdx.x].ref - from), sum);
+    const float log_sum = __builtin_amdgcn_logf(sum), loss = (log_sum - fmaf(at_label[t], kLog2e, -ref)) * kLn2;
     const int at = index ? index[t] : t;
-    p.lse[at] = lse;
-    p.loss[at] = lse - at_label[t];
+    p.lse[at] = fmaf(ref, kLn2, log_sum * kLn2);
+    p.loss[at] = loss < 0.f ? 0.f : loss;
 }
 
 // ---- gradient

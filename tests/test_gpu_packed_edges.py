@@ -76,3 +76,30 @@ def test_attention_of_more_sequences_than_a_workgroup_looks_at_once(precision, h
 def test_attention_of_groups_that_do_not_divide_a_tile(precision, heads, kv_heads, d, length):
     """Groups of 3, 5 and 6 heads in calls large enough for 128 rows a workgroup."""
     base.check_attention(base.run_attention(precision, heads, kv_heads, d, [(length, length), (33, 40)], True))
+
+
+@pytest.mark.parametrize("precision", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,v", [(5, 300), (64, 30), (200, 1000), (2048, 8200)])
+def test_vocab_loss_of_tokens_that_are_sure(precision, n, v):
+    """Large logits that float32 holds exactly, the label's often the largest: the loss has no error of the size of the logits' rounding steps (2^-7 here).
+
+    With D the distance of a logit from its token's largest, a weight is off by D (2^-26 for the constant log2e + 2^-24 for its argument) + 2^-23 for exp2, and the
+    label's argument by as much without exp2; the sum of v weights by (v / 64 + 72) 2^-24 and its logarithm by 2^-23 of itself.  D is at most 2 x 31.875 here."""
+    p, dt, _ = PRECISIONS[precision]
+    print(f"vocab loss {precision} {n} x 64 x {v}, sure", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(n + v)
+    x, w = torch.zeros(n, 64, device="cuda"), torch.zeros(v, 64, device="cuda")
+    x[:, 0], w[:, 0] = 1024.0, 125.0
+    x[:, 5] = 2.0 ** torch.randint(-1, 2, (n,), generator=gen, device="cuda")
+    w[:, 5] = -torch.randint(1, 256, (v,), generator=gen, device="cuda") / 8
+    w[v // 2, 5] = 0.0
+    labels = torch.randint(0, v, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    labels[::2] = v // 2
+    loss, lse = mt.op_vocab_loss(p, x.to(dt), w.to(dt), labels)
+    z = x.double() @ w.double().t()
+    want = torch.logsumexp(z - 128000.0, 1) - z[torch.arange(n, device="cuda"), labels.long()] + 128000.0
+    d = 63.75
+    bound = (v / 64 + 72) * 2.0 ** -24 + 2 * d * (2.0 ** -26 + 2.0 ** -24) + 2.0 ** -23 + 2.0 ** -22 * want
+    assert ((loss.double() - want).abs() <= bound).all(), (loss.double() - want).abs().max().item()
+    assert (loss >= 0).all()
+    assert ((lse.double() - torch.logsumexp(z, 1)).abs() <= 4 * 2.0 ** -24 * 128000).all()
