@@ -623,10 +623,15 @@ def _check(name, what, t, shape, dtype, gpu):
     _refuse(name, f"the last dimension of {what} is not contiguous")
 
 
+_MOST = 0x7FFFFFFF      # the entry points' sizes are 32-bit integers, to which ctypes cuts larger ones without a word
+
+
 def _dims(name, what, t, n):
     shape = t.shape
     if len(shape) != n:
         _refuse(name, f"{what} has {len(shape)} dimensions, not {n}")
+    if max(shape) > _MOST:
+        _refuse(name, f"{what} is {tuple(shape)}: sizes end at {_MOST}")
     return shape
 
 
@@ -650,6 +655,8 @@ def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, s
     """The checks and the call of both attention entry points; grads: (grad_ctx, grad_q, grad_k, grad_v)."""
     torch = _t()
     dt, gpu = _act_type(name, precision), q.get_device()
+    if scale is not None and not 0 < scale < 3.4e38:
+        _refuse(name, f"scale is {scale}")
     (tq, heads, d), (tk, kv_heads, _) = _dims(name, "q", q, 3), _dims(name, "k", k, 3)
     n_starts = _dims(name, "q_start", q_start, 1)
     key_shape = (tk, kv_heads, d)
@@ -765,6 +772,8 @@ def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add
     (n, h), (m,) = _dims(name, "grad", grad, 2), _dims(name, "ids", ids, 1)
     _check(name, "grad", grad, (m, h), dt, gpu)
     _check(name, "ids", ids, (m,), torch.int32, gpu)
+    if not 0 < vocab <= _MOST:
+        _refuse(name, f"a vocabulary of {vocab}")
     if add_to is None:
         out = torch.empty((vocab, h), dtype=torch.float32 if out_f32 else dt, device=grad.device)
     else:
