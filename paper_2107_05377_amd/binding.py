@@ -623,17 +623,20 @@ def _check(name, what, t, shape, dtype, gpu):
     _refuse(name, f"the last dimension of {what} is not contiguous")
 
 
-_MOST = 0x7FFFFFFF      # the entry points' sizes are 32-bit integers, to which ctypes cuts larger ones without a word
-
-
 def _dims(name, what, t, n):
     shape = t.shape
     if len(shape) != n:
         _refuse(name, f"{what} has {len(shape)} dimensions, not {n}")
-    if max(shape) > _MOST:
-        _refuse(name, f"{what} is {tuple(shape)}: sizes end at {_MOST}")
     return shape
 
+
+def _beyond(name, *sizes):
+    """The entry points' sizes are 32-bit integers, to which ctypes would cut larger ones without a word.  (Called where the sizes' bits say so.)"""
+    _refuse(name, f"sizes end at 2^31 - 1, these are {sizes}")
+
+
+# The stride of a dimension of one means nothing: torch calls such a tensor contiguous whatever it is, so the caller could not mend one that the entry points
+# refuse.  They are given one that they take.
 
 def _run(name, gpu, work_bytes, call):
     """call(work pointer, work bytes, stream) with a workspace of its own, on GPU `gpu` and its current stream."""
@@ -660,6 +663,8 @@ def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, s
     (tq, heads, d), (tk, kv_heads, _) = _dims(name, "q", q, 3), _dims(name, "k", k, 3)
     n_starts = _dims(name, "q_start", q_start, 1)
     key_shape = (tk, kv_heads, d)
+    if (tq | tk | heads | kv_heads | d | n_starts[0]) >> 31:
+        _beyond(name, tq, tk, heads, kv_heads, d, n_starts[0])
     _check(name, "q", q, q.shape, dt, gpu)
     _check(name, "k", k, key_shape, dt, gpu)
     _check(name, "v", v, key_shape, dt, gpu)
@@ -675,8 +680,17 @@ def _attention_call(name, entry, precision, q, k, v, q_start, k_start, causal, s
     if grads is not None:
         for what, t, like in zip(("grad_ctx", "grad_q", "grad_k", "grad_v"), grads, (q, q, k, k)):
             _check(name, what, t, like.shape, dt, gpu)
-        g_ptr, g_str = [t.data_ptr() for t in grads], [n for t in grads for n in t.stride()[:2]]
+        g_ptr = [t.data_ptr() for t in grads]
+        g_str = [0 if n == 1 else step for t in grads for step, n in zip(t.stride()[:2], t.shape)]
     (qr, qh, _), (kr, kh, _), (vr, vh, _), (cr, ch, _) = q.stride(), k.stride(), v.stride(), ctx.stride()
+    if tq == 1:
+        qr = cr = 0
+    if tk == 1:
+        kr = vr = 0
+    if heads == 1:
+        qh = ch = 0
+    if kv_heads == 1:
+        kh = vh = 0
 
     def pack(work, size):
         return _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), ctx.data_ptr(), 0 if lse is None else lse.data_ptr(), q_start.data_ptr(),
@@ -714,6 +728,8 @@ def _vocab_loss(name, precision, x, W, labels):
     torch = _t()
     dt, gpu = _act_type(name, precision), x.get_device()
     (n, h), (v, _) = _dims(name, "x", x, 2), _dims(name, "W", W, 2)
+    if (n | h | v) >> 31:
+        _beyond(name, n, h, v)
     _check(name, "x", x, (n, h), dt, gpu)
     _check(name, "W", W, (v, h), dt, gpu)
     _check(name, "labels", labels, (n,), torch.int32, gpu)
@@ -727,7 +743,8 @@ def op_vocab_loss(precision, x, W, labels):
     n, h, v, gpu = _vocab_loss("mt_op_vocab_loss", precision, x, W, labels)
     loss, lse = x.new_empty((2, n), dtype=torch.float32)
     _run("mt_op_vocab_loss", gpu, lib().mt_op_vocab_loss_work(precision, n, h, v, 0), lambda work, size, stream: lib().mt_op_vocab_loss(
-        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), n, h, v, work, size, stream))
+        precision, x.data_ptr(), x.stride(0) if n > 1 else h, W.data_ptr(), W.stride(0) if v > 1 else h, labels.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+        n, h, v, work, size, stream))
     return loss, lse
 
 
@@ -742,8 +759,8 @@ def op_vocab_loss_grad(precision, x, W, labels, lse, weight, out_f32=False):
     dx = torch.empty((n, h), dtype=x.dtype, device=x.device)
     dw = torch.empty((v, h), dtype=torch.float32 if out_f32 else x.dtype, device=x.device)
     _run(name, gpu, lib().mt_op_vocab_loss_work(precision, n, h, v, 1), lambda work, size, stream: lib().mt_op_vocab_loss_grad(
-        precision, x.data_ptr(), x.stride(0), W.data_ptr(), W.stride(0), labels.data_ptr(), lse.data_ptr(), weight.data_ptr(), dx.data_ptr(), dw.data_ptr(),
-        1 if out_f32 else 0, n, h, v, work, size, stream))
+        precision, x.data_ptr(), x.stride(0) if n > 1 else h, W.data_ptr(), W.stride(0) if v > 1 else h, labels.data_ptr(), lse.data_ptr(),
+        weight.data_ptr(), dx.data_ptr(), dw.data_ptr(), 1 if out_f32 else 0, n, h, v, work, size, stream))
     return dx, dw
 
 
@@ -752,6 +769,8 @@ def op_embedding(precision, table, ids, scale=1.0, out=None):
     name = "mt_op_embedding"
     dt, gpu = _act_type(name, precision), table.get_device()
     (n,), (v, h) = _dims(name, "ids", ids, 1), _dims(name, "table", table, 2)
+    if (n | h | v) >> 31:
+        _beyond(name, n, h, v)
     _check(name, "table", table, (v, h), dt, gpu)
     _check(name, "ids", ids, (n,), _t().int32, gpu)
     if out is None:
@@ -759,7 +778,7 @@ def op_embedding(precision, table, ids, scale=1.0, out=None):
     else:
         _check(name, "out", out, (n, h), dt, gpu)
     _run(name, gpu, 0, lambda work, size, stream: lib().mt_op_embedding(
-        precision, table.data_ptr(), table.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), n, v, h, stream))
+        precision, table.data_ptr(), table.stride(0) if v > 1 else h, ids.data_ptr(), scale, out.data_ptr(), out.stride(0) if n > 1 else h, n, v, h, stream))
     return out
 
 
@@ -772,15 +791,15 @@ def op_embedding_grad(precision, grad, ids, vocab, scale=1.0, out_f32=False, add
     (n, h), (m,) = _dims(name, "grad", grad, 2), _dims(name, "ids", ids, 1)
     _check(name, "grad", grad, (m, h), dt, gpu)
     _check(name, "ids", ids, (m,), torch.int32, gpu)
-    if not 0 < vocab <= _MOST:
-        _refuse(name, f"a vocabulary of {vocab}")
+    if (n | h | vocab) >> 31:
+        _beyond(name, n, h, vocab)
     if add_to is None:
         out = torch.empty((vocab, h), dtype=torch.float32 if out_f32 else dt, device=grad.device)
     else:
         out = add_to
         _check(name, "add_to", out, (vocab, h), torch.float32, gpu)
     _run(name, gpu, lib().mt_op_embedding_grad_work(precision, n, vocab, h), lambda work, size, stream: lib().mt_op_embedding_grad(
-        precision, grad.data_ptr(), grad.stride(0), ids.data_ptr(), scale, out.data_ptr(), out.stride(0), 1 if out.dtype is torch.float32 else 0,
+        precision, grad.data_ptr(), grad.stride(0) if n > 1 else h, ids.data_ptr(), scale, out.data_ptr(), out.stride(0) if vocab > 1 else h, 1 if out.dtype is torch.float32 else 0,
         0 if add_to is None else 1, n, vocab, h, work, size, stream))
     return out
 

@@ -103,3 +103,32 @@ def test_vocab_loss_of_tokens_that_are_sure(precision, n, v):
     assert ((loss.double() - want).abs() <= bound).all(), (loss.double() - want).abs().max().item()
     assert (loss >= 0).all()
     assert ((lse.double() - torch.logsumexp(z, 1)).abs() <= 4 * 2.0 ** -24 * 128000).all()
+
+
+def test_strides_of_dimensions_of_one():
+    """The stride of a dimension of one says nothing: whatever it is, the result is that of the same tensor laid out anew."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    p, dt = mt.MT_BF16, torch.bfloat16
+
+    def odd(t):                                              # the same values, 3 where a dimension is one
+        return t.as_strided(t.shape, [3 if n == 1 else s for s, n in zip(t.stride(), t.shape)])
+
+    for heads, kv_heads, n, m in ((4, 1, 1, 20), (1, 1, 1, 1), (1, 1, 9, 9), (4, 2, 1, 1)):
+        q, k, v, g = (normal(gen, r, h, 64, dtype=dt) for r, h in ((n, heads), (m, kv_heads), (m, kv_heads), (n, heads)))
+        qs, ks = starts([n]), starts([m])
+        ctx, lse = mt.op_packed_attention(p, q, k, v, qs, ks, want_lse=True)
+        grads = mt.op_packed_attention_grad(p, g, q, k, v, ctx, lse, qs, ks)
+        assert torch.equal(mt.op_packed_attention(p, odd(q), odd(k), odd(v), qs, ks, out=odd(torch.empty_like(ctx))), ctx)
+        got = mt.op_packed_attention_grad(p, odd(g), odd(q), odd(k), odd(v), odd(ctx), lse, qs, ks, out=[odd(torch.empty_like(t)) for t in grads])
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
+    ids, label, weight = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda")
+    for v in (1, 30):
+        x, w = normal(gen, 1, 64, dtype=dt), normal(gen, v, 64, dtype=dt)
+        loss, lse = mt.op_vocab_loss(p, x, w, label)
+        assert all(torch.equal(a, b) for a, b in zip(mt.op_vocab_loss(p, odd(x), odd(w), label), (loss, lse)))
+        grads = mt.op_vocab_loss_grad(p, x, w, label, lse, weight)
+        assert all(torch.equal(a, b) for a, b in zip(mt.op_vocab_loss_grad(p, odd(x), odd(w), label, lse, weight), grads))
+        assert torch.equal(mt.op_embedding(p, odd(w), ids, out=odd(torch.empty_like(x))), w[:1])
+        total = torch.zeros(v, 64, device="cuda")
+        mt.op_embedding_grad(p, odd(x), ids, v, add_to=odd(total))
+        assert torch.equal(total[:1], x.float())
