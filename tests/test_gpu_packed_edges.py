@@ -132,3 +132,18 @@ def test_strides_of_dimensions_of_one():
         total = torch.zeros(v, 64, device="cuda")
         mt.op_embedding_grad(p, odd(x), ids, v, add_to=odd(total))
         assert torch.equal(total[:1], x.float())
+
+
+@pytest.mark.parametrize("precision,n,h,v", [("bf16", 4160, 64, 70001), ("fp32", 4160, 128, 70001), ("fp32", 61, 64, 2100001), ("bf16", 70001, 64, 4111)])
+def test_vocab_loss_gradient_in_several_pieces(precision, n, h, v):
+    """More than 512 MB of dz: the vocabulary in pieces, whose dx is added up and whose last one is narrower."""
+    p, dt, u = PRECISIONS[precision]
+    assert -(-n // 64) * 64 * v * (2 if precision == "bf16" else 4) > 1 << 29
+    print(f"vocab loss in pieces {precision} {n} x {h} x {v}", flush=True)
+    x, w, labels, weight = base.make_loss(precision, n, h, v, 0.9)
+    want, bound = base.loss_formula(x, w, labels, weight, u)
+    loss, lse = mt.op_vocab_loss(p, x, w, labels)
+    within(loss, want["loss"], bound["loss"], "loss")
+    dx, dw = mt.op_vocab_loss_grad(p, x, w, labels, lse, weight)
+    within(dx, want["dx"], bound["dx"], "dx")
+    within(dw, want["dw"], bound["dw"] + 1.01 * (u + 2 * base.E) * want["dw"].abs(), "dw")
