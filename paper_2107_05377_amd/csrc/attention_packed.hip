@@ -342,11 +342,6 @@ __device__ __forceinline__ void clear_columns(unsigned char* t, int rows, int d)
 
 // The tiles that pass by go through a ring in LDS: one is used while up to STAGES - 1 are under way.  All loads of a loop are those of its ring, LPS of each
 // wavefront per tile, so that a wait can leave the last tiles under way.
-template <int N>
-__device__ __forceinline__ void wait_loads()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 template <int STAGES, int LPS>
 __device__ __forceinline__ void tile_landed(int behind)         // tiles behind this one that have been asked for
 {

@@ -395,7 +395,6 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(Embedding p, Sums s
     put_row<Out, N>(p, id, c, out);
 }
 
-size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 int chunks_of(int n) { return (n + kChunk - 1) / kChunk; }
 // keys of a thread of the sort: 4 spread the work over more workgroups, but each adds up the counts of all.  Whole gradient with 4 and with 16: 32768 tokens 39.3 and
 // 60.6 us, 131072 60.2 and 76.6, 400000 128.7 and 122.6

@@ -9,6 +9,9 @@ namespace mt {
 // a launch has less than 2^32 threads
 inline bool fits_launch(int64_t groups, int threads) { return groups >= 0 && groups * threads < 1ll << 32; }
 
+// bytes of a workspace's part
+inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
 // ---- attention over packed sequences.  Strides in elements; rows of a head are `d` contiguous elements.
 struct PackedAttn {
     const void *q, *k, *v;

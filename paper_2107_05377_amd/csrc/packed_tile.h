@@ -54,6 +54,13 @@ __device__ __forceinline__ void load_to_lds_4(const void* from, uint32_t to)
 }
 #pragma clang diagnostic pop
 
+// all but the wavefront's last N loads have landed
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // ---- element types: what 16 bytes of a row mean to the matrix instructions
 struct B16 {
     typedef __bf16 elem;

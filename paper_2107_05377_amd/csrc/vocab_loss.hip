@@ -110,12 +110,6 @@ struct Stager {
     }
 };
 
-template <int N>
-__device__ __forceinline__ void wait_loads()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
 // A workgroup's BM x BN block of a product: WM x WN wavefronts of TMI x TNI blocks of 32 x 32; acc[i][j]: block i of the first operand's rows (registers),
 // j of the second's (lanes).  Slices of BK elements of the sum go through a ring of STAGES in LDS, straight from memory; the barrier of a slice stands in
 // its last step, when its operands are in registers, so that the next slice's first operands are read behind that step's matrix instructions.
@@ -531,8 +525,6 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabLoss p, const i
         *reinterpret_cast<out4*>(dx + (int64_t)to * p.hidden + c) = o;
     }
 }
-
-size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The kind of blocks, by the bound on the tokens (the count of the labelled ones is known on the device alone).  Measured on both sides (30522 x 768, us):
 //   FEW instead of MID: 5 tokens 15.3, not 20.1; 64 tokens 16.8, not 21.9 (float32 39, not 66; gradient 71.9, not 78.5).  128 tokens 22.7, not 23.0, but
