@@ -147,3 +147,97 @@ def test_vocab_loss_gradient_in_several_pieces(precision, n, h, v):
     dx, dw = mt.op_vocab_loss_grad(p, x, w, labels, lse, weight)
     within(dx, want["dx"], bound["dx"], "dx")
     within(dw, want["dw"], bound["dw"] + 1.01 * (u + 2 * base.E) * want["dw"].abs(), "dw")
+
+
+# ---- offsets that 32 bits do not hold
+
+def test_attention_of_keys_beyond_4_gb():
+    """A sequence whose keys lie more than 4 GB (and 2^31 elements) into the cache: forward pass and gradient are those of the same sequence alone."""
+    p, dt = mt.MT_BF16, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    far, n = (1 << 24) + 77, 700
+    q, g = normal(gen, 3, 4, 64, dtype=dt), normal(gen, 3, 4, 64, dtype=dt)
+    k, v = (torch.zeros(far + n, 2, 64, dtype=dt, device="cuda") for _ in range(2))
+    k[far:], v[far:] = normal(gen, n, 2, 64, dtype=dt), normal(gen, n, 2, 64, dtype=dt)
+    qs, ks = torch.tensor([0, 0, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, far, far + n], dtype=torch.int32, device="cuda")
+    want = mt.op_packed_attention(p, q, k[far:].clone(), v[far:].clone(), starts([3]), starts([n]), want_lse=True)
+    got = mt.op_packed_attention(p, q, k, v, qs, ks, want_lse=True)
+    # (keys may be dealt out otherwise: sums of 700 terms in another order, weights rounded about another reference)
+    assert ((got[0].double() - want[0].double()).abs() <= 2.0 ** -7 * (1 + want[0].double().abs())).all()
+    assert ((got[1] - want[1]).abs() <= 2.0 ** -20 * (1 + want[1].abs())).all()
+    alone = mt.op_packed_attention_grad(p, g, q, k[far:].clone(), v[far:].clone(), *want, starts([3]), starts([n]))
+    grads = mt.op_packed_attention_grad(p, g, q, k, v, *want, qs, ks)
+    assert torch.equal(grads[0], alone[0])
+    for a, b in zip(grads[1:], alone[1:]):
+        assert torch.equal(a[far:], b) and (a[:far:4099] == 0).all()
+
+
+def test_embedding_beyond_4_gb():
+    p, dt = mt.MT_BF16, torch.bfloat16
+    v, h = (1 << 22) + 9, 1024
+    table = torch.zeros(v, h, dtype=dt, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    table[-5:] = normal(gen, 5, h, dtype=dt)
+    ids = torch.tensor([v - 1, 0, v - 5, v - 3, v - 1], dtype=torch.int32, device="cuda")
+    assert torch.equal(mt.op_embedding(p, table, ids), table[ids.long()])
+    grad = normal(gen, 5, h, dtype=dt)
+    out = mt.op_embedding_grad(p, grad, ids, v)
+    assert torch.equal(out[v - 5], grad[2]) and torch.equal(out[v - 3], grad[3]) and torch.equal(out[v - 1], (grad[0].float() + grad[4].float()).to(dt))
+    assert (out[v - 2] == 0).all() and (out[1:v - 5:4099] == 0).all() and torch.equal(out[0], grad[1])
+
+
+def test_vocab_loss_of_weights_beyond_4_gb():
+    """Columns of zeros but for the last rows of the weights: their logits, gradients of x and of these rows are those of a small vocabulary with as many zeros
+    reckoned in."""
+    p, dt, u = PRECISIONS["bf16"]
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n, h, v, last = 70, 1024, (1 << 21) + 300, 299
+    x = normal(gen, n, h, dtype=dt)
+    w = torch.zeros(v, h, dtype=dt, device="cuda")
+    w[-last:] = (normal(gen, last, h, dtype=torch.float32) / 4).to(dt)            # logits of +-8
+    labels = torch.randint(v - last, v, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    weight = torch.randn(n, generator=gen, device="cuda") / n
+    z = x.double() @ w[-last:].double().t()
+    lse = torch.logsumexp(torch.cat([z, torch.full((n, 1), math.log(v - last), dtype=torch.float64, device="cuda")], 1), 1)
+    at = (labels.long() - (v - last))[:, None]
+    loss, got_lse = mt.op_vocab_loss(p, x, w, labels)
+    # z to (h + 8) 2^-24 of its terms (sum of 1024 terms of 0.2: 1.3e-2), the sums of 2^21 equal weights in ranges of 128 and then in slices: 2^-24 x (128 + 2^21 / 128 / 16)
+    e = 2 * (h + 8) * 2.0 ** -24 * (x.double().abs() @ w[-last:].double().abs().t()).amax(1) + (128 + 1100) * 2.0 ** -24 + 2.0 ** -21 * (1 + z.abs().amax(1))
+    assert ((got_lse.double() - lse).abs() <= e + 2.0 ** -22 * lse).all()
+    assert ((loss.double() - (lse - z.gather(1, at)[:, 0])).abs() <= 2 * e + 2.0 ** -22 * lse).all()
+    dx, dw = mt.op_vocab_loss_grad(p, x, w, labels, got_lse, weight)
+    dz = torch.exp(z - lse[:, None])
+    dz.scatter_add_(1, at, torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda"))
+    dz *= weight.double()[:, None]
+    ez = (2 * e[:, None] + u) * (dz.abs() + (torch.exp(z - lse[:, None]) * weight.double().abs()[:, None]))
+    within(dx, dz @ w[-last:].double(), 1.01 * (ez @ w[-last:].double().abs() + (u + 4 * base.E) * (dz @ w[-last:].double()).abs()), "dx")
+    want = dz.t() @ x.double()
+    within(dw[-last:], want, 1.01 * (ez.t() @ x.double().abs() + (u + 4 * base.E) * want.abs()) + (n + 8) * base.E * (dz.abs().t() @ x.double().abs()), "dw")
+    zero = (torch.exp(-lse) * weight.double()) @ x.double()
+    size = (torch.exp(-lse) * weight.double().abs()) @ x.double().abs()
+    within(dw[:v - last:40961], zero.expand(len(dw[:v - last:40961]), h), ((u + 2 * e.amax() + (n + 8) * base.E) * size + u * zero.abs()).expand(len(dw[:v - last:40961]), h), "dw of zeros")
+
+
+def test_captured_single_tokens_whose_lengths_change():
+    """Two graphs of dealt-out keys in one pool, each replayed over other lengths than those it was captured with: the bits of the eager calls."""
+    p, dt = mt.MT_BF16, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    heads, kv_heads, total = 16, 4, 20000
+    lengths = [[5000, 1, 0, 700, 9000, 64, 300, 1200], [0, 0, 19000, 1, 1, 1, 500, 497], [2500] * 8, [1] * 8]
+    q, k, v = normal(gen, 8, heads, 128, dtype=dt), normal(gen, total, kv_heads, 128, dtype=dt), normal(gen, total, kv_heads, 128, dtype=dt)
+    qs, tables = starts([1] * 8), [starts(n) for n in lengths]
+    eager = [[t.clone() for t in mt.op_packed_attention(p, q, k, v, qs, t, want_lse=True)] for t in tables]
+    live = [tables[0].clone(), tables[1].clone()]
+    graphs, outs = [], []
+    for t in live:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=graphs[0].pool() if graphs else None):
+            outs.append(mt.op_packed_attention(p, q, k, v, qs, t, want_lse=True))
+        graphs.append(graph)
+    for turn in range(6):
+        for i in (0, 1):
+            live[i].copy_(tables[(turn + i) % 4])
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], eager[(turn + i) % 4])), (turn, i)
+            mt.op_packed_attention(p, q, k, v, qs, tables[turn % 4])
