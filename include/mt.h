@@ -437,11 +437,12 @@ int mt_op_layernorm(const float* d_x, const float* d_gamma, const float* d_beta,
                     void* d_out_bf16, int32_t M, int32_t H, void* hip_stream);
 
 /*
- * Operators on packed tokens: what the students of the merged model are trained with before they are merged (Sections 3.1 and 3.2: fine-tuning and
- * distillation), and attention for prompts and single tokens of any length.  MT_BF16 (activations, weights and gradients bfloat16, sums float32) or
- * MT_FP32_CHECK (all float32); other precisions: MT_ERR_CONFIG.  Tensors and row strides (in elements) are 16-byte aligned, workspaces 256-byte; a
- * workspace holds nothing between calls, and calls that may overlap need one each.  hip_stream belongs to the current device.  No atomics on
- * sums: equal inputs give equal bits.  Errors: NULL, CONFIG, SHAPE (also: a workspace smaller than the *_work function says), HIP.
+ * Operators on packed tokens, for language models beside the serving pass (which calls none of them): attention for prompts and single tokens of any
+ * length, a loss over the vocabulary and an embedding, each with its gradient.  MT_BF16 (activations, weights and gradients bfloat16, sums float32) or
+ * MT_FP32_CHECK (all float32); other precisions: MT_ERR_CONFIG.  Every size is at least one.  Tensors and row strides (in elements) are 16-byte aligned,
+ * workspaces 256-byte; a workspace holds nothing between calls, and calls that may overlap need one each.  Results overlap neither one another nor anything
+ * that is read, but for grad_table with accumulate.  hip_stream belongs to the current device.  No atomics on sums: equal inputs give equal bits.  Errors:
+ * NULL, CONFIG, SHAPE (also: a workspace smaller than the *_work function says), HIP.
  */
 /* Attention over n_seqs (at most 16384) packed sequences.   Sequence b owns query rows d_q_start[b] .. d_q_start[b+1]-1 and key rows d_k_start[b] .. d_k_start[b+1]-1
  * (device int32 [n_seqs + 1], not falling; starts outside [0, total] are brought inside; d_k_start NULL: the queries').  With Lq queries and Lk keys,
@@ -450,7 +451,7 @@ int mt_op_layernorm(const float* d_x, const float* d_gamma, const float* d_beta,
  *   P = softmax(scale q k^T) over the keys seen, ctx = P v, lse = log sum exp(scale q k^T);  a query that sees no key: ctx 0, lse -infinity.
  * Keys that a query does not see never reach it, whatever they hold; rows of no sequence are neither read nor written.
  * Row r of head a of tensor t is `width` contiguous elements at t + r * t_row + a * t_head (results: rows within heads or heads within rows, none
- * overlapping); width: a multiple of 8 up to 128; scale > 0.
+ * overlapping); width: a multiple of 8 up to 128; scale > 0; total_k and total_q * heads / kv_heads up to 2^29, total_q * heads up to 2^34.
  * lse: float32 [heads][total_q].  MT_BF16 rounds P, and dS in the gradient, to bfloat16 where they enter the second products. */
 typedef struct mt_packed_attention {
     const void *d_q, *d_k, *d_v;
@@ -473,19 +474,20 @@ int mt_op_packed_attention_grad(const mt_packed_attention* op, void* hip_stream)
 size_t mt_op_packed_attention_work(const mt_packed_attention* op, int32_t grad);
 
 /* Softmax cross entropy of z = x W^T over a vocabulary, which never stores z.  d_x [tokens][ldx], d_W [vocab][ldw], hidden columns each (a multiple of
- * 64); d_labels int32 [tokens]:  lse_i = log sum_v exp z_iv, loss_i = lse_i - z_i,label  (float32 [tokens], not averaged).  A label outside
+ * 64 up to 2^20); d_labels int32 [tokens]:  lse_i = log sum_v exp z_iv, loss_i = lse_i - z_i,label  (float32 [tokens], not averaged).  A label outside
  * [0, vocab) means none: its token's row reaches nothing, whatever it holds; its loss, lse and gradient are 0.  vocab at most 2^22, tokens 2^23. */
 int mt_op_vocab_loss(int32_t precision, const void* d_x, int64_t ldx, const void* d_W, int64_t ldw, const int32_t* d_labels, float* d_loss, float* d_lse,
                      int32_t tokens, int32_t hidden, int32_t vocab, void* d_work, size_t work_bytes, void* hip_stream);
 /* dz_iv = weight_i (exp(z_iv - lse_i) - [v = label_i]), d_grad_x = dz W [tokens][hidden], d_grad_W = dz^T x [vocab][hidden] (dense, written whole;
  * float32 with grad_W_f32 != 0).  d_lse: mt_op_vocab_loss's; d_weight float32 [tokens]: the gradient of each token's loss (1 / labelled tokens: their
- * mean).  MT_BF16 rounds dz to bfloat16 where it enters the two products. */
+ * mean).  MT_BF16 rounds dz to bfloat16 where it enters the two products, whatever type grad_W has.  The workspace holds dz of a piece of the vocabulary,
+ * for all tokens: up to 512 MB, or 1024 entries a token where those are more. */
 int mt_op_vocab_loss_grad(int32_t precision, const void* d_x, int64_t ldx, const void* d_W, int64_t ldw, const int32_t* d_labels, const float* d_lse,
                           const float* d_weight, void* d_grad_x, void* d_grad_W, int32_t grad_W_f32, int32_t tokens, int32_t hidden, int32_t vocab,
                           void* d_work, size_t work_bytes, void* hip_stream);
 size_t mt_op_vocab_loss_work(int32_t precision, int32_t tokens, int32_t hidden, int32_t vocab, int32_t grad);
 
-/* out_i = scale * table[id_i]; an id outside [0, vocab): a row of zeros.  hidden: a multiple of 8 (float32: of 4).  d_table [vocab][ldt], d_out [n][ldo]. */
+/* out_i = scale * table[id_i]; an id outside [0, vocab): a row of zeros.  hidden: a multiple of 8 (float32: of 4) up to 2^16; n, vocab up to 2^28.  d_table [vocab][ldt], d_out [n][ldo]. */
 int mt_op_embedding(int32_t precision, const void* d_table, int64_t ldt, const int32_t* d_ids, float scale, void* d_out, int64_t ldo, int32_t n,
                     int32_t vocab, int32_t hidden, void* hip_stream);
 /* The table's gradient (n at most 2^24): d_grad_table[v] = scale * sum over i with id_i = v of d_grad[i], float32 sums; zeros for rows without a token.

@@ -584,7 +584,8 @@ def op_layernorm(x, gamma, beta, eps, want_bf16=False):
 
 
 # ---- operators on packed tokens.  A call of few tokens takes the device a few microseconds, so what stands between it and the library is kept short:
-# one comparison for each thing that is checked, texts only for what is refused, the argument struct packed in one go.
+# one comparison for each thing that is checked, texts only for what is refused, the argument struct packed in one go.  They are plain calls: no result carries
+# a history for torch's autograd, whatever its operands require; gradients are what the *_grad calls return.  An empty batch is refused, as by the model.
 
 def _refuse(name, text, code=MT_ERR_SHAPE):
     raise MTError(code, f"{name}: {text}")

@@ -17,11 +17,15 @@
 // Nothing that a row does not see reaches it: scores are replaced, not multiplied by zero, and in blocks that a mask cuts, a non-finite first
 // operand is kept out of the product and put back for the rows that see it.
 //
-// What bounds it (MI355X, bfloat16 unless said otherwise).  Forward, 8192 tokens, 32 heads on 8 of D = 128, causal: 540 us, 1.02 PFLOP/s, matrix and vector
-// instructions (exp, maximum, rounding of P) in turn.  D = 64 has half the matrix work for the same softmax: vector instructions, 16 heads on 4 over documents
-// of 300..4001 tokens: forward 104 us, gradient 335 us.  256 sentences of 16..128 tokens, twelve heads: 35 us, start-up of a workgroup that has one or two key
-// blocks.  Single tokens against a cache of 100..8191 keys: 39 us for 125 MB, 3.2 TB/s, where a copy of that size reaches 4.8.  float32: its matrix
-// instructions have a sixteenth of the rate; forward and gradient of 7 sequences of 60..509 tokens, a few hundred workgroups: 120 us.
+// What bounds it (MI355X, bfloat16 unless said otherwise; times of whole calls among others, shares of a call and busy pipes from a profiler).  Forward, 8192
+// tokens, 32 heads on 8 of D = 128, causal: 548 us, 1.00 PFLOP/s, matrix and vector instructions (exp, maximum, rounding of P) in turn, 48 % of the cycles each.
+// D = 64 has half the matrix work for the same softmax: 16 heads on 4 over 9 documents of 300..4001 tokens, forward and gradient 451 us, of which the forward
+// pass is 22 % (vector instructions 66 %, matrix 33 % of its cycles), dq 30 % (56 and 36), dk and dv 45 % (37 and 31, with two
+// wavefronts per SIMD), delta 4 %.  256 sentences of 16..128 tokens, twelve heads: 35 us, start-up of a workgroup that has one or two key blocks (matrix 8 %).
+// Single tokens against a cache of 100..8191 keys: 39 us for 125 MB, 3.2 TB/s, where a copy of that size reaches 4.7.  float32: its matrix instructions have
+// a sixteenth of the rate; forward and gradient of 7 sequences of 60..509 tokens, a few hundred workgroups: 121 us.
+// Heads between 64 and 128 columns do the matrix work of 128, those below 64 that of 64: the documents with D = 128 845 us, 80 785, 32 390 on a card
+// where D = 64 takes 434.
 #include "packed_tile.h"
 #include "packed.h"
 
@@ -709,7 +713,7 @@ __global__ __launch_bounds__(256) void packed_stat_kernel(PackedAttn p, float* s
 }
 
 // dq: rows fixed, keys pass by.  RW blocks of 32 rows, each with KW wavefronts that take a block of 32 keys of a tile each.  Three products (S, dP, dq) for one
-// exp: documents of 300..4001 tokens, 16 heads on 4 of D = 64, 144 us; matrix and vector instructions.
+// exp: documents of 300..4001 tokens, 16 heads on 4 of D = 64, 147 us under the profiler; vector and matrix instructions.
 // Rounding: in bfloat16 dS is rounded to the operands' type before the last product (half a step, 2^-9 .. 2^-8 of each term), as P is in the forward pass.
 template <typename E, int DP, int RW, int KW, int STAGES>
 struct RowGrad {
@@ -820,7 +824,7 @@ __global__ __launch_bounds__(RW * KW * 64, (waves_of<E, DP>(3))) void packed_dq_
 }
 
 // dk, dv: keys fixed, the rows of all heads of the group pass by.  KW blocks of 32 keys, each with RW wavefronts that take one block of 32 rows of a tile
-// each and put their sums together at the end.  Four products (S, dP, dv, dk): the documents above 217 us.  For D = 64 one block of keys with four wavefronts of rows
+// each and put their sums together at the end.  Four products (S, dP, dv, dk): the documents above 220 us.  For D = 64 one block of keys with four wavefronts of rows
 // (each with a quarter of the rows and all sums of its keys in registers) instead of two by two: whole gradient and forward pass 566 -> 519 us.
 // Rounding: P and dS to the operands' type, as above; the sums over the heads of a group stay in float32.
 template <typename E, int DP, int KW, int RW, int STAGES>
@@ -975,14 +979,15 @@ __global__ __launch_bounds__(KW * RW * 64, (Tile<E, DP>::ROWB == 128 ? 2 : 1)) v
 // us; q: queries of a sequence, k: its keys, D: columns of a head):
 //   32 rows, four wavefronts (D = 128: two) that share the keys, for rows of one query.  With 64 rows and two of them instead: 128 x 12 heads of D = 64 with
 //     20..61 keys 14.2, not 19.8; 200..500 keys 30.4, not 32.3; 1000..2000 keys 111, not 110; 300 x 4 key heads of D = 128 with 1000..3000 keys 222, not 218;
-//     float32 with 200..500 keys 111, not 101.  Hence from 256 keys per sequence on, and always with few workgroups, whose keys may be dealt out (below),
-//     because a long sequence among short ones would hold up the launch: short ones alone (64 sequences of 8..28 keys) would take 10.3, not 12.5.
+//     float32 with 200..500 keys 111, not 101.  Hence from 256 keys per sequence on, for both types: bfloat16 alone would have 64 rows up to about 1000 keys, where
+//     they gain 6 per cent at most, float32 alone 32 rows from fewer keys on.  Always with few workgroups, whose keys may be dealt out (below), because a
+//     long sequence among short ones would hold up the launch: short ones alone (64 sequences of 8..28 keys) would take 10.3, not 12.5.
 //   64 rows, two wavefronts of rows by two that share the keys, for short sequences (20..60 tokens 9.8; 128 rows 10.8) and few tiles (512 tokens x 4, four
 //     key heads 12.1; 14.2.  1000 tokens, twelve 16.7; 21.0.  1000 tokens, eight of D = 128 with groups of 4 23.6; 30.6).
 //   128 rows, four wavefronts, each with its own rows and all the keys, so that each key block is read from LDS for twice the rows: 512 tokens x 8, four key
 //     heads 16.0; 64 rows 19.4.  256 x 64 tokens, twelve heads 31.4; 35.1, 256 x 30..80 36; 38.  64 x 128 tokens, twelve heads, 15.1; 19.6.  9 sequences of 300..4001 tokens 111; 131.  8192 tokens, D = 128 560; 698.
 //   Keys dealt out to several workgroups, whose sums a second launch joins: one token over 8192 keys, eight heads 17.5; not dealt out 114.
-//     32 tokens over 100..8191 keys 33.8; 115.
+//     32 tokens over 100..8191 keys 33.8; 115.  Only for 32 rows: what has more rows a sequence walks all keys in each workgroup, however few those are.
 struct Deal {
     int rows_each;          // rows of a workgroup: 32, 64 or 128
     int keys_each;          // > 0: keys of a workgroup

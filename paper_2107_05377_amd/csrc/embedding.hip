@@ -1,7 +1,7 @@
 // Rows of an embedding table, scaled, and the table's gradient.
 //   out_i = scale table[id_i] (an id outside the vocabulary: zeros),  dtable_v = scale sum over i with id_i = v of grad_i, in the order of i
 // Both move memory and little else: 32768 tokens of width 768 in bfloat16 are looked up in 13.7 us (50 MB read, most of it from caches, and 50 MB written), and
-// their gradient over 30522 rows in float32 takes 65 us: the sort's launches 21, sums and cleared rows 26 (144 MB, 5.5 TB/s), the join of cut runs 5, and the gaps between.
+// their gradient over 30522 rows in float32 takes 70 us: the sort's launches 21, sums and cleared rows 25 (144 MB, 5.7 TB/s), the join of cut runs 5, and the gaps between.
 //
 // Gradient.  The tokens are sorted by id, keeping their order (radix sort of (id, place) pairs, 8 bits or fewer a pass, no atomics whose order could
 // show), and cut into chunks of kChunk sorted tokens, whatever ids they have: words follow a 1 / rank law, so a workgroup per table row would leave

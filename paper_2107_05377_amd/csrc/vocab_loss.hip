@@ -6,11 +6,13 @@
 // has as many rows (dW: as long a sum) as there are.  Forward: blocks of z are multiplied, reduced to a maximum and a sum of exponentials per
 // token and range of the vocabulary, and the ranges are joined.  Gradient: for a piece of the vocabulary at a time dz is formed from z multiplied
 // again (bfloat16: rounded to bfloat16, half a step of 2^-8 per term, as any operand of these products) and used for both gradients.  Multiplying again costs a
-// quarter of the work; keeping z in float32 would move 4 bytes for every 2 x hidden operations, twice, and hold tokens x vocab x 4 bytes.
+// quarter of the work and holds nothing between the two calls; keeping z in float32 would move 4 bytes for every 2 x hidden operations, twice, and hold
+// tokens x vocab x 4 bytes: more time in bfloat16 up to a hidden size of about 1000, less in float32 (at 768 10 ps of products a logit against 2 of memory).
 //
-// What bounds it (MI355X).  Many tokens: the matrix rate; 4099 x 1024 x 128000, 97 % labelled, 4.2 ms for 4 products, 0.99 PFLOP/s (a library's product of
-// 8192^3: 1.23).  8192 tokens of which 15 % are labelled, 768 x 30522: 330 us; 600 blocks of 256 x 256 on 256 compute units leave the last round a third full.
-// 5 tokens: one pass over the weights, 47 MB in 10 us, 4.7 TB/s, and a join of 4 us.  float32, 509 tokens, 768 x 30522: 820 us, 116 TFLOP/s (a library's 8192^3: 154).
+// What bounds it (MI355X).  Many tokens: the matrix rate; 4099 x 1024 x 128000, 97 % labelled, 4.2 ms for 4 products, 0.98 PFLOP/s (a library's product of
+// 8192^3: 1.21), matrix instructions 41 to 66 % of the kernels' cycles.  8192 tokens of which 15 % are labelled, 768 x 30522: 339 us; 600 blocks of 256 x 256 on 256
+// compute units leave the last round a third full.  5 tokens: one pass over the weights, 47 MB in 10 us, 4.5 TB/s, and a join of 4 us.  float32, 509 tokens,
+// 768 x 30522: 825 us, 116 TFLOP/s (a library's 8192^3: 153).
 #include "packed_tile.h"
 #include "packed.h"
 
@@ -559,7 +561,7 @@ Plan grad_plan(int tokens, int hidden, int vocab)
 {
     const size_t es = E::SIZE, rows = (size_t)(tokens + 63) / 64 * 64;
     Plan p;
-    // pieces of the vocabulary: dz of at most 512 MB
+    // pieces of the vocabulary: dz of at most 512 MB, or of 1024 entries where those are more (from 2^18 tokens on in bfloat16, 2^17 in float32; then 2 or 4 KB a token)
     const size_t fit = (size_t)(512u << 20) / (rows * es) / 256 * 256, whole = ((size_t)vocab + 255) / 256 * 256;
     p.piece = (int)std::min(whole, std::max<size_t>(fit, 1024));
     const int kind = blocks_for<E>(tokens, vocab), bm = kind == BIG ? 256 : 128, bn = kind == BIG ? 256 : kind == MID ? 128 : 32, h_blocks = (hidden + bm - 1) / bm;
