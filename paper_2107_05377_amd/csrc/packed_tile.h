@@ -23,11 +23,14 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0");
 }
-// a pointer that is the same in all lanes, in scalar registers
+// A pointer that is the same in all lanes, in scalar registers.  Behind a vector instruction that writes one, a load has to wait 5 states before it reads it, which
+// the compiler sees to in its own code only: here the wait is part of the value (where that is scalar work already, as in all kernels so far, 5 cycles a tile).
 __device__ __forceinline__ const char* uniform(const char* p)
 {
     const uint64_t v = (uint64_t)(uintptr_t)p;
-    return reinterpret_cast<const char*>((uintptr_t)((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v)));
+    uint64_t s = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v);
+    asm("s_nop 4" : "+s"(s));
+    return reinterpret_cast<const char*>((uintptr_t)s);
 }
 // the same from a place that all lanes share and a lane's offset in bytes
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to)
